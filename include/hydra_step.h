@@ -1,0 +1,106 @@
+/*
+ * hydra_step.h - what a step of a serving instance does around the attention of hydra_attn.h, on MI355X (gfx950).
+ *
+ *   hydra_page_maps_build   the step's control arrays, built on the GPU from request lengths: cache blocks for the new tokens off a
+ *                           free list, block tables, cache slots, positions, packed offsets, context lengths
+ *   hydra_qk_norm_rope      queries and keys of one layer: norm of every head, rotation by positions with one or several axes
+ *                           (time, height, width), and K and V into the paged cache, in one pass
+ *
+ * The arrays are those of hydra_attn.h: bf16 tokens [tokens, heads, head_dim] with a token stride, int32 lengths and tables, int64
+ * slots, caches [num_blocks, block_size, n_kv_heads, head_dim].  So are the conventions: device pointers owned by the caller, work
+ * enqueued on `stream`, no allocation, no synchronisation, results that are bit-identical from run to run, a hydra_status for every
+ * argument error that the host can see, before anything is launched.  A call may be recorded into a HIP graph.  The calls run on
+ * the current device, which has to be that of `stream` and of the arrays.
+ */
+#ifndef HYDRA_STEP_H
+#define HYDRA_STEP_H
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include "hydra_attn.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/*
+ * Page maps of one step.
+ *
+ * Request b has context_lens[b] tokens in the cache, in the blocks that its row of the block table names, and brings q_lens[b] new
+ * ones (0: none in this step).  With P = block_size, held = ceil(context / P) and need = ceil((context + q) / P) - held, the requests
+ * take their new blocks in the order of the batch from the end of the free list:
+ *     end_b = need_0 + .. + need_b;   request b is served if need_b == 0 or end_b <= n_free
+ *     block_tables[b, held + j] = free_blocks[n_free - 1 - (end_b - need_b + j)]      for a served request and 0 <= j < need_b
+ * so from the first request on that the list has too few blocks for, only requests that need none are served.  A request whose
+ * context is negative or whose tokens would not fit its row of the table (context + q > max_blocks_per_seq * P) is not served, and
+ * takes part in no sum but that of the tokens; a negative q counts as 0.  Then
+ *     cu_seqlens_q[b] = q_0 + .. + q_(b-1)                                           [batch + 1]
+ *     kv_lens[b]      = context + q if served, 0 otherwise                           [batch]
+ *     next_context[b] = context + q if served, context otherwise                     [batch], may be NULL, may be context_lens itself
+ *     token t = cu_seqlens_q[b] + i of request b, at key position p = context + i:
+ *       slot_mapping[t] = block_tables[b, p / P] * P + p % P if served, -1 otherwise [total_tokens]
+ *       positions[t]    = p + position_deltas[b]                                     [total_tokens], may be NULL
+ *     pool[0] = blocks left on the list, pool[1] = blocks that it lacked             [2]; pool[0] may be *n_free itself
+ * are what hydra_kv_cache_write, hydra_qk_norm_rope, hydra_attn_paged_fwd and hydra_attn_prefix_fwd take.  A request that was not
+ * served writes nothing into the cache and gets no attention output (its kv_len is below its q_len).
+ *
+ *   total_tokens  length of slot_mapping and positions, at least the sum of q_lens; entries behind the last token become -1 and 0
+ *        (a recorded graph's buffers may be longer than the step's tokens).  At most 2^20.  Where the sum is larger, cu_seqlens_q stays
+ *        at total_tokens and the requests whose tokens do not fit are not served.
+ *   free_blocks   device int32 [free_capacity], the first *n_free of them free; *n_free is taken as 0 .. free_capacity.
+ *   block_tables  device int32 [batch, max_blocks_per_seq], read and written in place.
+ *   position_deltas  device int32 [batch] or NULL (all 0): what a request's positions are ahead of its keys, as behind an image whose
+ *        tokens share positions.
+ *   block_size    a power of two, at least 1.  num_blocks * block_size below 2^31.  A block outside 0 .. num_blocks - 1, in the table or
+ *        on the list, gives slot -1.
+ *   batch at most 65535, max_blocks_per_seq * block_size at most 2^30.
+ * Arrays must not overlap but as said.  batch == 0 returns HYDRA_OK without launching.
+ */
+int hydra_page_maps_build(const int32_t* q_lens, const int32_t* context_lens, int32_t* block_tables, int32_t max_blocks_per_seq,
+                          const int32_t* free_blocks, int32_t free_capacity, const int32_t* n_free, const int32_t* position_deltas,
+                          int32_t batch, int32_t total_tokens, int32_t block_size, int64_t num_blocks,
+                          int32_t* cu_seqlens_q, int32_t* kv_lens, int64_t* slot_mapping, int32_t* positions, int32_t* next_context,
+                          int32_t* pool, void* stream);
+
+/*
+ * Norm and rotation of queries and keys, and the cache write.
+ *
+ * For every token t and every head row x of q (weight w = q_weight) and of k (w = k_weight), with d = head_dim, R = rotary_dim:
+ *     norm      x_j <- x_j * w_j / sqrt(mean_j(x_j^2) + eps)                          (w NULL: x as it is)
+ *     rotation  for pair i in 0 .. R/2 - 1:  a = positions[freq_axis[i], t] * inv_freq[i],
+ *               (x_l, x_u) <- (x_l cos a - x_u sin a,  x_u cos a + x_l sin a)
+ *               l, u = i, i + R/2 (interleaved == 0) or 2 i, 2 i + 1 (interleaved != 0); elements from R on stay
+ * in fp32, rounded to bf16 once (nearest even).  The product of position and frequency is reduced exactly to a part of a turn
+ * (64-bit fixed point), so that far positions lose nothing.
+ * The rows go to q_out and k_out; and, with caches, for s = slot_mapping[t] in 0 .. num_blocks * block_size - 1
+ *     k_cache[s / block_size, s % block_size, :, :] = the rows of k,   v_cache[..] = v[t, :, :] (bit copy)
+ * (tokens with another slot are not written there, as in hydra_kv_cache_write; no two tokens share a slot).
+ *
+ *   q, k, v   bf16 [total_tokens, heads, head_dim], token strides in elements, multiples of 8, 16-byte aligned; may be views into
+ *             one fused buffer.  v only with caches.
+ *   q_out, k_out  the same with strides of their own; may be q and k themselves (same address, same stride), but overlap no other
+ *             array.  k_out may be NULL with caches.
+ *   q_weight, k_weight  bf16 [head_dim], 16-byte aligned, or NULL.  eps finite and >= 0.  The sum of squares is taken in fp32: values of
+ *             2^60 and more in a row that is normalised overflow it.
+ *   positions device int32, axis a at positions + a * position_axis_stride, one per token; any int32.  A stride of 0 gives every axis
+ *             the same positions.  n_axes 1 .. 4.
+ *   inv_freq  device fp32 [R / 2], finite.   freq_axis  device int32 [R / 2], values clamped to 0 .. n_axes - 1, or NULL (all 0).
+ *   rotary_dim a multiple of 16, 0 .. head_dim; 0: no rotation (positions, inv_freq are not read and may be NULL).
+ *   head_dim  64, 80 or 128.  n_q_heads and n_kv_heads at least 1, n_q_heads + 2 n_kv_heads at most 65535.
+ *   k_cache, v_cache, slot_mapping  all or none (NULL); contiguous, 16-byte aligned.  block_size >= 1; block_size * num_blocks is the
+ *             number of slots.
+ * total_tokens at most 2^25; 0 returns HYDRA_OK without launching.
+ */
+int hydra_qk_norm_rope(const void* q, const void* k, const void* v, int64_t q_token_stride, int64_t k_token_stride, int64_t v_token_stride,
+                       void* q_out, void* k_out, int64_t q_out_token_stride, int64_t k_out_token_stride,
+                       const void* q_weight, const void* k_weight, float eps,
+                       const int32_t* positions, int64_t position_axis_stride, int32_t n_axes,
+                       const float* inv_freq, const int32_t* freq_axis, int32_t rotary_dim, int32_t interleaved,
+                       void* k_cache, void* v_cache, const int64_t* slot_mapping, int32_t block_size, int64_t num_blocks,
+                       int32_t total_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* HYDRA_STEP_H */

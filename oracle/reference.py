@@ -250,3 +250,65 @@ def page_cache_gather(cache_bits, slot_mapping, rows_bits):
             raise ValueError("slot out of range")
         rows[t] = flat[slot]
     return rows
+
+
+def page_maps(q_lens, context_lens, block_tables, free_blocks, n_free, total_tokens: int, block_size: int, num_blocks: int, position_deltas=None):
+    """One step's page maps, request by request: (cu_seqlens_q, kv_lens, slot_mapping, positions, next_context, pool, block_tables)."""
+    tables = np.array(block_tables, dtype=np.int64)
+    width = tables.shape[1]
+    n_free = min(max(int(n_free), 0), len(free_blocks))
+    left, wanted, shut = n_free, 0, False
+    cu, kv, nxt = [0], [], []
+    slots = np.full(total_tokens, -1, dtype=np.int64)
+    positions = np.zeros(total_tokens, dtype=np.int64)
+    at = 0  # tokens so far
+    for b, (q, context) in enumerate(zip(q_lens, context_lens)):
+        q, context = max(int(q), 0), int(context)
+        delta = 0 if position_deltas is None else int(position_deltas[b])
+        fits = context >= 0 and context + q <= width * block_size
+        inside = q == 0 or at + q <= total_tokens
+        held = -(-context // block_size) if fits else 0
+        need = -(-(context + q) // block_size) - held if fits else 0
+        served = fits and inside
+        if served and need > 0:
+            wanted += need
+            shut = shut or wanted > n_free  # nobody behind the first one that cannot be served gets a new block
+            served = not shut
+            if served:
+                for j in range(need):
+                    left -= 1
+                    tables[b, held + j] = free_blocks[left]
+        for i in range(q):
+            t = at + i
+            if t >= total_tokens:
+                break
+            p = context + i
+            positions[t] = p + delta
+            if served:
+                block = tables[b, p // block_size]
+                if 0 <= block < num_blocks:
+                    slots[t] = block * block_size + p % block_size
+        at = min(at + q, total_tokens)
+        cu.append(at)
+        kv.append(context + q if served else 0)
+        nxt.append(context + q if served else context)
+    return cu, kv, slots, positions, nxt, [left, max(wanted - n_free, 0)], tables
+
+
+def qk_norm_rope(x, weight, eps: float, positions, inv_freq, freq_axis, interleaved: bool) -> np.ndarray:
+    """Norm (weight None: none) and rotation of x [tokens, heads, d] in fp64; positions int [axes, tokens], inv_freq [pairs] (may be
+    empty), freq_axis int [pairs] or None."""
+    x = np.array(x, dtype=np.float64)
+    if weight is not None:
+        x = x / np.sqrt((x * x).mean(axis=-1, keepdims=True) + eps) * np.asarray(weight, dtype=np.float64)
+    out = x.copy()
+    pairs = len(inv_freq)
+    for i in range(pairs):
+        axis = 0 if freq_axis is None else min(max(int(freq_axis[i]), 0), len(positions) - 1)
+        # (whole turns are taken off in long double, so that the angle of a far position keeps the fp64 digits)
+        turns = np.asarray(positions[axis], dtype=np.longdouble) * np.longdouble(inv_freq[i]) / (2 * np.longdouble("3.14159265358979323846264338327950288"))
+        a = np.asarray((turns - np.rint(turns)) * (2 * np.longdouble("3.14159265358979323846264338327950288")), dtype=np.float64)[:, None]
+        l, u = (2 * i, 2 * i + 1) if interleaved else (i, i + pairs)
+        out[:, :, l] = x[:, :, l] * np.cos(a) - x[:, :, u] * np.sin(a)
+        out[:, :, u] = x[:, :, u] * np.cos(a) + x[:, :, l] * np.sin(a)
+    return out

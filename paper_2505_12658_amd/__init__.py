@@ -1,7 +1,8 @@
-"""MI355X-native packed variable-length attention, paged KV-cache write and attention over the paged cache (gfx950 HIP kernels
-behind a C ABI; this package is only the thin Python binding)."""
+"""MI355X-native packed variable-length attention, paged KV-cache write and attention over the paged
+cache, and what a serving step does around them (gfx950 HIP kernels behind a C ABI; this package is only the thin Python binding)."""
 from .binding import (  # noqa: F401
     HydraError,
+    PageMaps,
     hydra_attn_build_worklist,
     hydra_attn_paged_fwd,
     hydra_attn_paged_workspace_bytes,
@@ -13,6 +14,8 @@ from .binding import (  # noqa: F401
     hydra_kv_cache_write,
     hydra_page_cache_gather,
     hydra_page_cache_write,
+    hydra_page_maps_build,
+    hydra_qk_norm_rope,
     hydra_status_string,
     library_path,
     load_library,

@@ -1,4 +1,4 @@
-"""Python binding of include/hydra_attn.h.  Argument marshalling only, in native code (csrc/torch_binding.cpp):
+"""Python binding of include/hydra_attn.h and include/hydra_step.h.  Argument marshalling only, in native code (csrc/torch_binding.cpp):
 tensors in, raw device pointers and sizes out; every step of the computation runs in the HIP kernels.  There is no
 fallback: if the shared library or its binding is missing, loading raises."""
 from __future__ import annotations
@@ -6,7 +6,7 @@ from __future__ import annotations
 import ctypes
 import importlib.util
 import os
-from typing import Optional
+from typing import NamedTuple, Optional, Tuple
 
 import torch
 
@@ -61,6 +61,11 @@ def load_library() -> ctypes.CDLL:
         lib.hydra_page_cache_write.argtypes = [vp, i64, vp, vp, i32, i32, i64, vp]
         lib.hydra_page_cache_gather.restype = ctypes.c_int
         lib.hydra_page_cache_gather.argtypes = [vp, vp, vp, i64, i32, i32, i64, vp]
+        lib.hydra_page_maps_build.restype = ctypes.c_int
+        lib.hydra_page_maps_build.argtypes = [vp, vp, vp, i32, vp, i32, vp, vp, i32, i32, i32, i64, vp, vp, vp, vp, vp, vp, vp]
+        lib.hydra_qk_norm_rope.restype = ctypes.c_int
+        lib.hydra_qk_norm_rope.argtypes = [vp, vp, vp, i64, i64, i64, vp, vp, i64, i64, vp, vp, ctypes.c_float, vp, i64, i32, vp, vp, i32, i32, vp, vp, vp, i32, i64,
+                                           i32, i32, i32, i32, vp]
         lib.hydra_attn_workspace_bytes.restype = sz
         lib.hydra_attn_workspace_bytes.argtypes = [i32] * 6
         lib.hydra_status_string.restype = ctypes.c_char_p
@@ -152,3 +157,46 @@ def hydra_page_cache_write(rows: torch.Tensor, cache: torch.Tensor, slot_mapping
 def hydra_page_cache_gather(cache: torch.Tensor, slot_mapping: torch.Tensor, rows: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
     """cache rows at slot_mapping -> rows [n, row_elems] bf16 (row-strided view allowed); rows with a negative slot keep their contents."""
     _calls().page_cache_gather(cache, slot_mapping, rows, stream)
+
+
+class PageMaps(NamedTuple):
+    """What hydra_page_maps_build writes, for a batch of B requests; all on the GPU."""
+    cu_seqlens_q: torch.Tensor           # int32 [B + 1]
+    kv_lens: torch.Tensor                # int32 [B]
+    slot_mapping: torch.Tensor           # int64 [total_tokens]
+    positions: Optional[torch.Tensor]    # int32 [total_tokens]
+    next_context: Optional[torch.Tensor] # int32 [B]
+    pool: torch.Tensor                   # int32 [2]: blocks left on the free list, blocks that it lacked
+
+
+def hydra_page_maps_build(q_lens: torch.Tensor, context_lens: torch.Tensor, block_tables: torch.Tensor, free_blocks: torch.Tensor, n_free: torch.Tensor,
+                          total_tokens: int, block_size: int, num_blocks: int, position_deltas: Optional[torch.Tensor] = None,
+                          maps: Optional[PageMaps] = None, stream: Optional[torch.cuda.Stream] = None) -> PageMaps:
+    """Takes cache blocks for q_lens (int32 [B]) new tokens behind context_lens (int32 [B]) off the end of the first n_free (int32 [1]) of
+    free_blocks (int32), into block_tables (int32 [B, max_blocks_per_seq], in place), and returns the step's maps.  maps: buffers to
+    write them into (allocated if None); its next_context may be context_lens and its pool begin with n_free, for a state that moves on in place."""
+    if maps is None:
+        batch = q_lens.numel()
+
+        def empty(n, dtype=torch.int32):
+            t = torch.empty(n, dtype=dtype, device=q_lens.device)
+            if stream is not None:
+                t.record_stream(stream)
+            return t
+
+        maps = PageMaps(empty(batch + 1), empty(batch), empty(total_tokens, torch.int64), empty(total_tokens), empty(batch), empty(2))
+    _calls().page_maps_build(q_lens, context_lens, block_tables, free_blocks, n_free, total_tokens, block_size, num_blocks, position_deltas, *maps, stream)
+    return maps
+
+
+def hydra_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: Optional[torch.Tensor], inv_freq: Optional[torch.Tensor],
+                       freq_axis: Optional[torch.Tensor] = None, q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None,
+                       eps: float = 1e-6, interleaved: bool = False, q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
+                       v: Optional[torch.Tensor] = None, k_cache: Optional[torch.Tensor] = None, v_cache: Optional[torch.Tensor] = None,
+                       slot_mapping: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """q [N, Hq, d], k and v [N, Hkv, d] bf16 (token-strided views allowed): every head normalised with q_weight / k_weight (bf16 [d], None: not),
+    rotated by positions (int32 [N] or [axes, N]) times inv_freq (fp32 [rotary_dim / 2], None: not), frequency i on axis freq_axis[i] (int32, None: the
+    first), pairs (i, i + rotary_dim / 2) or with `interleaved` (2 i, 2 i + 1).  Returns (q_out, k_out): the tensors given (q and k
+    themselves for in place), or new ones.  With caches [num_blocks, block_size, Hkv, d] the rows of k, and v's as they are, go to slot_mapping (int64 [N], < 0 skips)
+    there, and to k_out only if it is given (None is returned otherwise)."""
+    return _calls().qk_norm_rope(q, k, positions, inv_freq, freq_axis, q_weight, k_weight, eps, interleaved, q_out, k_out, v, k_cache, v_cache, slot_mapping, stream)

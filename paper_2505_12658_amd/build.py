@@ -10,9 +10,11 @@ import os
 import subprocess
 import sys
 import sysconfig
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-SRC = os.path.join(HERE, "csrc", "hydra_api.hip")
+SOURCES = [os.path.join(HERE, "csrc", name) for name in ("hydra_api.hip", "hydra_step.hip")]
 LIB = os.path.join(HERE, "libhydra_attn.so")
 BINDING_SRC = os.path.join(HERE, "csrc", "torch_binding.cpp")
 BINDING = os.path.join(HERE, "_hydra_torch.so")
@@ -23,7 +25,6 @@ HIPCC_FLAGS = [
     "-std=c++17",
     # packed fp32 VALU forms are kept out of the generated code
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-    "-shared",
     "-fPIC",
 ]
 
@@ -53,8 +54,13 @@ def _binding_command():
 
 
 def build(verbose: bool = False) -> str:
-    _run([os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")] + HIPCC_FLAGS + [SRC, "-o", LIB], verbose)
-    _run(_binding_command(), verbose)
+    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+    with tempfile.TemporaryDirectory() as tmp:
+        objects = [os.path.join(tmp, os.path.basename(source) + ".o") for source in SOURCES]
+        commands = [[hipcc] + HIPCC_FLAGS + ["-c", source, "-o", obj] for source, obj in zip(SOURCES, objects)] + [_binding_command()]
+        with ThreadPoolExecutor(len(commands)) as pool:
+            list(pool.map(lambda command: _run(command, verbose), commands))
+        _run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC"] + objects + ["-o", LIB], verbose)
     return LIB
 
 

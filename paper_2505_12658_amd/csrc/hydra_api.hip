@@ -5,7 +5,6 @@
 #include <stdint.h>
 
 #include <atomic>
-#include <tuple>
 #include <type_traits>
 
 #include "../../include/hydra_attn.h"
@@ -13,6 +12,7 @@
 #include "attn_paged.hpp"
 #include "batch_rules.hpp"
 #include "kv_write.hpp"
+#include "launch.hpp"
 #include "page_cache.hpp"
 #include "worklist.hpp"
 
@@ -22,27 +22,7 @@ static_assert(hydra::rules::kTileTokens == hydra::kWaveTileRows && hydra::rules:
 
 namespace {
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-bool head_dim_supported(int d) { return d == 64 || d == 80 || d == 128; }
-
-// Enqueues one kernel and returns the status of THIS launch (the runtime's sticky last-error slot
-// is shared by every caller of the process and may hold somebody else's failure).
-template <typename... Params, typename... Args>
-hipError_t launch_lds(void (*kernel)(Params...), dim3 grid, dim3 block, size_t lds_bytes, hipStream_t stream, const Args&... args) {
-  static_assert(sizeof...(Params) == sizeof...(Args), "one argument per kernel parameter");
-  std::tuple<Params...> vals(args...);
-  return std::apply(
-      [&](auto&... v) {
-        void* ptrs[] = {static_cast<void*>(&v)...};
-        return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, block, ptrs, lds_bytes, stream);
-      },
-      vals);
-}
-template <typename... Params, typename... Args>
-hipError_t launch(void (*kernel)(Params...), dim3 grid, dim3 block, hipStream_t stream, const Args&... args) {
-  return launch_lds(kernel, grid, block, 0, stream, args...);
-}
+using hydra::aligned16, hydra::head_dim_supported, hydra::launch, hydra::launch_lds;
 
 // A row-copy kernel (its form for rows of whole kilobytes, its form for others) over `rows` rows of row16 pieces: one launch,
 // or several where a grid cannot hold them.

@@ -1,0 +1,162 @@
+// C ABI of include/hydra_step.h: argument validation on the host, then launches.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "../../include/hydra_step.h"
+#include "launch.hpp"
+#include "page_maps.hpp"
+#include "qk_rope.hpp"
+
+using hydra::aligned16, hydra::head_dim_supported, hydra::launch;
+
+namespace {
+
+// log2 of a cache's block size; -1 if it is no power of two, or the cache or a row of the block table is larger than the calls
+// take (rows of the cache have 31-bit numbers).
+int block_shift_of(int32_t block_size, int64_t num_blocks, int32_t max_blocks_per_seq) {
+  if (block_size < 1 || (block_size & (block_size - 1)) != 0) return -1;
+  if (num_blocks > 0x7fffffff / block_size || (int64_t)max_blocks_per_seq * block_size > (int64_t)1 << 30) return -1;
+  int shift = 0;
+  while ((1 << shift) < block_size) ++shift;
+  return shift;
+}
+
+}  // namespace
+
+extern "C" {
+
+int hydra_page_maps_build(const int32_t* q_lens, const int32_t* context_lens, int32_t* block_tables, int32_t max_blocks_per_seq,
+                          const int32_t* free_blocks, int32_t free_capacity, const int32_t* n_free, const int32_t* position_deltas,
+                          int32_t batch, int32_t total_tokens, int32_t block_size, int64_t num_blocks,
+                          int32_t* cu_seqlens_q, int32_t* kv_lens, int64_t* slot_mapping, int32_t* positions, int32_t* next_context,
+                          int32_t* pool, void* stream) {
+  namespace maps = hydra::maps;
+  if (batch < 0 || total_tokens < 0 || free_capacity < 0 || num_blocks < 0 || max_blocks_per_seq < 0 || block_size < 1) return HYDRA_ERR_INVALID_ARG;
+  const int shift = block_shift_of(block_size, num_blocks, max_blocks_per_seq);
+  if (shift < 0 || batch > 65535 || total_tokens > maps::kMostTokens) return HYDRA_ERR_UNSUPPORTED;
+  if (batch == 0) return HYDRA_OK;
+  if (!q_lens || !context_lens || !n_free || !cu_seqlens_q || !kv_lens || !pool) return HYDRA_ERR_INVALID_ARG;
+  if ((max_blocks_per_seq > 0 && !block_tables) || (free_capacity > 0 && !free_blocks) || (total_tokens > 0 && !slot_mapping)) return HYDRA_ERR_INVALID_ARG;
+
+  maps::Args args;
+  args.q_lens = q_lens;
+  args.context_lens = context_lens;
+  args.block_tables = block_tables;
+  args.free_blocks = free_blocks;
+  args.n_free = n_free;
+  args.position_deltas = position_deltas;
+  args.cu_seqlens_q = cu_seqlens_q;
+  args.kv_lens = kv_lens;
+  args.slot_mapping = slot_mapping;
+  args.positions = positions;
+  args.next_context = next_context;
+  args.pool = pool;
+  args.free_capacity = free_capacity;
+  args.max_blocks_per_seq = max_blocks_per_seq;
+  args.batch = batch;
+  args.total_tokens = total_tokens;
+  args.block_shift = shift;
+  args.num_blocks = (int32_t)num_blocks;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const unsigned grid = total_tokens > 0 ? (unsigned)((total_tokens + maps::kTokensPerWorkgroup - 1) / maps::kTokensPerWorkgroup) : 1u;
+  const dim3 block(maps::kThreads);
+  hipError_t err;
+  if (grid > 1 && (next_context == context_lens || pool == n_free)) {
+    err = launch(maps::page_maps_kernel<true, false>, dim3(grid), block, s, args);
+    if (err == hipSuccess) err = launch(maps::page_maps_kernel<false, true>, dim3(1), block, s, args);
+  } else {
+    err = launch(maps::page_maps_kernel<true, true>, dim3(grid), block, s, args);
+  }
+  return err == hipSuccess ? HYDRA_OK : HYDRA_ERR_LAUNCH;
+}
+
+int hydra_qk_norm_rope(const void* q, const void* k, const void* v, int64_t q_token_stride, int64_t k_token_stride, int64_t v_token_stride,
+                       void* q_out, void* k_out, int64_t q_out_token_stride, int64_t k_out_token_stride,
+                       const void* q_weight, const void* k_weight, float eps,
+                       const int32_t* positions, int64_t position_axis_stride, int32_t n_axes,
+                       const float* inv_freq, const int32_t* freq_axis, int32_t rotary_dim, int32_t interleaved,
+                       void* k_cache, void* v_cache, const int64_t* slot_mapping, int32_t block_size, int64_t num_blocks,
+                       int32_t total_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, void* stream) {
+  namespace rope = hydra::rope;
+  if (total_tokens < 0 || n_q_heads <= 0 || n_kv_heads <= 0 || rotary_dim < 0) return HYDRA_ERR_INVALID_ARG;
+  if (!head_dim_supported(head_dim) || rotary_dim % 16 != 0) return HYDRA_ERR_UNSUPPORTED;
+  if ((int64_t)n_q_heads + 2 * (int64_t)n_kv_heads > 65535 || total_tokens > 1 << 25) return HYDRA_ERR_UNSUPPORTED;
+  if (rotary_dim > head_dim || !(eps >= 0.0f) || isinf(eps)) return HYDRA_ERR_INVALID_ARG;
+  const bool cached = k_cache || v_cache || slot_mapping;
+  if (cached && (!k_cache || !v_cache || !slot_mapping || !v)) {
+    if (total_tokens > 0) return HYDRA_ERR_INVALID_ARG;
+  }
+  if (cached && (block_size < 1 || num_blocks < 0)) return HYDRA_ERR_INVALID_ARG;
+  if (rotary_dim > 0 && n_axes < 1) return HYDRA_ERR_INVALID_ARG;
+  if (rotary_dim > 0 && n_axes > rope::kMostAxes) return HYDRA_ERR_UNSUPPORTED;
+  if (total_tokens == 0) return HYDRA_OK;
+  if (!q || !k || !q_out || (!k_out && !cached)) return HYDRA_ERR_INVALID_ARG;
+  if (rotary_dim > 0 && (!positions || !inv_freq || position_axis_stride < 0)) return HYDRA_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out) || !aligned16(q_weight) || !aligned16(k_weight) || !aligned16(k_cache) ||
+      !aligned16(v_cache) || (cached && !aligned16(v)))
+    return HYDRA_ERR_INVALID_ARG;
+  const int64_t q_row = (int64_t)n_q_heads * head_dim, kv_row = (int64_t)n_kv_heads * head_dim;
+  if (q_token_stride < q_row || q_out_token_stride < q_row || k_token_stride < kv_row || (k_out && k_out_token_stride < kv_row) || (cached && v_token_stride < kv_row))
+    return HYDRA_ERR_INVALID_ARG;
+  if ((q_token_stride | q_out_token_stride | k_token_stride | (k_out ? k_out_token_stride : 0) | (cached ? v_token_stride : 0)) & 7) return HYDRA_ERR_INVALID_ARG;
+
+  if ((q_out == q && q_out_token_stride != q_token_stride) || (k_out == k && k_out_token_stride != k_token_stride)) return HYDRA_ERR_INVALID_ARG;
+
+  rope::Args args;
+  args.q = static_cast<const uint16_t*>(q);
+  args.k = static_cast<const uint16_t*>(k);
+  args.v = static_cast<const uint16_t*>(v);
+  args.q_out = static_cast<uint16_t*>(q_out);
+  args.k_out = static_cast<uint16_t*>(k_out);
+  args.k_cache = static_cast<uint16_t*>(k_cache);
+  args.v_cache = static_cast<uint16_t*>(v_cache);
+  args.q_stride = q_token_stride;
+  args.k_stride = k_token_stride;
+  args.v_stride = cached ? v_token_stride : 0;
+  args.q_out_stride = q_out_token_stride;
+  args.k_out_stride = k_out_token_stride;
+  args.q_weight = static_cast<const uint16_t*>(q_weight);
+  args.k_weight = static_cast<const uint16_t*>(k_weight);
+  args.positions = positions;
+  args.axis_stride = position_axis_stride;
+  args.inv_freq = inv_freq;
+  args.freq_axis = freq_axis;
+  args.slot_mapping = slot_mapping;
+  args.num_slots = cached ? num_blocks * block_size : 0;
+  args.eps = eps;
+  args.n_axes = n_axes;
+  args.rotary_pieces = rotary_dim / 16;
+  args.interleaved = interleaved;
+  args.total_tokens = total_tokens;
+  args.n_q_heads = n_q_heads;
+  args.n_kv_heads = n_kv_heads;
+  args.n_rows = n_q_heads + n_kv_heads + (cached ? n_kv_heads : 0);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  auto launch_for = [&](auto d, auto norm) {
+    constexpr int D = decltype(d)::value;
+    constexpr bool kNorm = decltype(norm)::value;
+    constexpr int kRows = rope::kRowsPerWave<D, kNorm>;
+    // Few tokens: as many waves as there are loads of rows, so that every wave has one trip to memory and back.
+    constexpr int64_t kWavesWanted = 4096;
+    const int loads = (args.n_rows + kRows - 1) / kRows;
+    const int64_t wanted = kWavesWanted / total_tokens;
+    const int parts = wanted < 1 ? 1 : (wanted < loads ? (int)wanted : loads);
+    args.rows_per_part = (loads + parts - 1) / parts * kRows;
+    args.parts = (args.n_rows + args.rows_per_part - 1) / args.rows_per_part;
+    const int64_t waves = (int64_t)total_tokens * args.parts;
+    return launch(rope::qk_norm_rope_kernel<D, kNorm>, dim3((unsigned)((waves + rope::kWaves - 1) / rope::kWaves)), dim3(64 * rope::kWaves), s, args);
+  };
+  using std::bool_constant, std::integral_constant;
+  auto launch_dim = [&](auto norm) {
+    switch (head_dim) {
+      case 64: return launch_for(integral_constant<int, 64>{}, norm);
+      case 80: return launch_for(integral_constant<int, 80>{}, norm);
+      default: return launch_for(integral_constant<int, 128>{}, norm);
+    }
+  };
+  const hipError_t err = q_weight || k_weight ? launch_dim(bool_constant<true>{}) : launch_dim(bool_constant<false>{});
+  return err == hipSuccess ? HYDRA_OK : HYDRA_ERR_LAUNCH;
+}
+
+}  // extern "C"

@@ -1,0 +1,156 @@
+// Page maps of a step: blocks off the free list, block tables, slots, positions, offsets and context lengths (include/hydra_step.h).
+//
+// Two sums run over the requests, of new tokens and of new blocks; everything else follows from a request's place in them.  Every
+// workgroup takes both sums over the whole batch, 1024 requests at a time, a request per thread, and keeps the piece that
+// its own tokens lie in; a token then finds its request by a search in LDS.  So one launch does, without a second one that would wait
+// for the sums of a first: the lengths are some KB that every workgroup after the first finds in L2.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "wave_ops.hpp"
+
+namespace hydra {
+namespace maps {
+
+constexpr int kThreads = 1024;
+constexpr int kWaves = kThreads / 64;
+constexpr int kTokensPerWorkgroup = 2048;
+constexpr int kMostTokens = 1 << 20;  // per step: 1024 requests' sums of lengths that are held to one more than this fit 31 bits
+
+struct Args {
+  const int32_t* q_lens;
+  const int32_t* context_lens;
+  int32_t* block_tables;
+  const int32_t* free_blocks;
+  const int32_t* n_free;
+  const int32_t* position_deltas;
+  int32_t* cu_seqlens_q;
+  int32_t* kv_lens;
+  int64_t* slot_mapping;
+  int32_t* positions;
+  int32_t* next_context;
+  int32_t* pool;
+  int32_t free_capacity, max_blocks_per_seq, batch, total_tokens, block_shift, num_blocks;
+};
+
+// grid: a workgroup per kTokensPerWorkgroup tokens.  TOKENS: tokens, tables and what a request gets; STATE: next_context and pool.
+// Both in one launch unless several workgroups would still read what they overwrite (the same arrays as context_lens and n_free).
+template <bool TOKENS, bool STATE>
+__global__ __launch_bounds__(kThreads) void page_maps_kernel(const Args a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __shared__ int32_t s_end[kThreads], s_context[kThreads], s_first[kThreads];  // per request: end of its tokens, context, place of its first new block on the list
+  __shared__ int32_t s_wave[2][kWaves];
+  __shared__ int32_t s_taken, s_wanted;  // blocks off the list, and blocks that all the requests of the step need
+  const int thread = (int)threadIdx.x, lane = thread & 63, wave = thread >> 6;
+  const int n_free_given = *a.n_free;
+  const int n_free = n_free_given < 0 ? 0 : (n_free_given > a.free_capacity ? a.free_capacity : n_free_given);
+  const int in_block = (1 << a.block_shift) - 1;
+  const int begin = (int)blockIdx.x * kTokensPerWorkgroup;
+  const int end = begin + kTokensPerWorkgroup < a.total_tokens ? begin + kTokensPerWorkgroup : a.total_tokens;
+  if (thread == 0) s_taken = s_wanted = 0;
+  int tokens_before = 0, blocks_before = 0;  // of the requests of earlier rounds
+  for (int first = 0; first < a.batch; first += kThreads) {
+    const int b = first + thread;
+    int q = 0, context = 0;
+    if (b < a.batch) {
+      q = a.q_lens[b];
+      context = a.context_lens[b];
+    }
+    q = q < 0 ? 0 : (q > kMostTokens ? kMostTokens + 1 : q);
+    const bool fits_row = context >= 0 && (int64_t)context + q <= (int64_t)a.max_blocks_per_seq << a.block_shift;
+    const int held = fits_row ? (int)(((int64_t)context + in_block) >> a.block_shift) : 0;
+    const int need = fits_row ? (int)(((int64_t)context + q + in_block) >> a.block_shift) - held : 0;  // (no more than q)
+    int q_end = wave_scan_add(q), need_end = wave_scan_add(need);
+    if (lane == 63) {
+      s_wave[0][wave] = q_end;
+      s_wave[1][wave] = need_end;
+    }
+    __syncthreads();
+    int q_round = 0, need_round = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const int qw = s_wave[0][w], nw = s_wave[1][w];
+      q_end += w < wave ? qw : 0;
+      need_end += w < wave ? nw : 0;
+      q_round += qw;
+      need_round += nw;
+    }
+    q_end += tokens_before;
+    need_end += blocks_before;
+    const bool in_step = q == 0 || q_end <= a.total_tokens;
+    const bool served = fits_row && in_step && (need == 0 || need_end <= n_free);
+    const int token_end = q_end < a.total_tokens ? q_end : a.total_tokens;
+    if (STATE) {
+      // (sums only grow, and those that are served with new blocks come before those that are not)
+      if (need > 0 && served) atomicMax(&s_taken, need_end);
+      if (need > 0 && in_step) atomicMax(&s_wanted, need_end);
+      if (a.next_context && blockIdx.x == 0 && b < a.batch) a.next_context[b] = served ? context + q : context;
+    }
+    if (TOKENS) {
+      if (blockIdx.x == 0 && b < a.batch) {
+        a.cu_seqlens_q[b + 1] = token_end;
+        a.kv_lens[b] = served ? context + q : 0;
+        if (b == 0) a.cu_seqlens_q[0] = 0;
+      }
+      s_end[thread] = token_end;
+      s_context[thread] = context;
+      s_first[thread] = served ? n_free - 1 - (need_end - need) : -1 - (1 << 30);
+    }
+    __syncthreads();
+    if (TOKENS) {
+      const int round_begin = tokens_before > begin ? tokens_before : begin;
+      int round_end = tokens_before + q_round;
+      round_end = round_end < end ? round_end : end;
+      const int in_round = a.batch - first < kThreads ? a.batch - first : kThreads;
+      for (int t = round_begin + thread; t < round_end; t += kThreads) {
+        // the first request that ends behind token t
+        int lo = 0, hi = in_round - 1;
+        while (lo < hi) {
+          const int mid = (lo + hi) >> 1;
+          if (s_end[mid] > t) hi = mid;
+          else lo = mid + 1;
+        }
+        const int start = lo > 0 ? s_end[lo - 1] : tokens_before;
+        const int of = first + lo, held_tokens = s_context[lo], at = s_first[lo];
+        const int position = (int)((uint32_t)held_tokens + (uint32_t)(t - start));
+        int64_t slot = -1;
+        if (at >= -1 - kMostTokens) {  // served  (the place may be below 0 only where no new block is needed)
+          const int page = position >> a.block_shift, held_pages = (int)(((int64_t)held_tokens + in_block) >> a.block_shift);
+          int32_t* entry = a.block_tables + (int64_t)of * a.max_blocks_per_seq + page;
+          int block;
+          if (page >= held_pages) {
+            block = a.free_blocks[at - (page - held_pages)];
+            if ((position & in_block) == 0) *entry = block;  // (every new block begins with a new token)
+          } else {
+            block = *entry;
+          }
+          if (block >= 0 && block < a.num_blocks) slot = ((int64_t)block << a.block_shift) + (position & in_block);
+        }
+        a.slot_mapping[t] = slot;
+        if (a.positions) a.positions[t] = (int)((uint32_t)position + (a.position_deltas ? (uint32_t)a.position_deltas[of] : 0u));
+      }
+    }
+    tokens_before += q_round;
+    tokens_before = tokens_before < a.total_tokens ? tokens_before : a.total_tokens;
+    blocks_before += need_round;
+    blocks_before = blocks_before < 1 << 29 ? blocks_before : 1 << 29;  // (more only where the tokens are beyond total_tokens)
+    __syncthreads();
+  }
+  if (TOKENS) {
+    for (int t = (tokens_before > begin ? tokens_before : begin) + thread; t < end; t += kThreads) {
+      a.slot_mapping[t] = -1;
+      if (a.positions) a.positions[t] = 0;
+    }
+  }
+  if (STATE && blockIdx.x == 0 && thread == 0) {
+    a.pool[0] = n_free - s_taken;
+    a.pool[1] = s_wanted > n_free ? s_wanted - n_free : 0;
+  }
+#else
+  (void)a;
+#endif
+}
+
+}  // namespace maps
+}  // namespace hydra

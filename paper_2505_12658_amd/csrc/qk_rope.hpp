@@ -1,0 +1,235 @@
+// Norm of every head of q and k, rotation by position, and the rows of K and V into the paged cache (include/hydra_step.h).
+//
+// One wave takes the head rows of one token, or a part of them where there are few tokens: q's, k's and v's one after the other, as
+// many at a time as its lanes hold.  A lane has two 16-byte pieces of a row that are half of the rotated part apart, so that both
+// elements of each of its eight pairs are its own, in either order of pairs (elements i and i + R/2: one from each piece;
+// 2 i and 2 i + 1: neighbours).  All rows of a token rotate by the same angles: a lane computes its eight sines and cosines once.
+//
+// Angles: frequency / 2 pi is a fixed-point part of a turn (64 bits, whole turns dropped); times the position, modulo 2^64, that is exact
+// to position * 2^-62 turns, and its upper half, as a signed 32-bit part of a turn, goes to the sine, whose argument is in turns.
+//
+// What bounds it: HBM, each row is read once and written once; with a handful of tokens the two trips to memory.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "attn_tiles.hpp"
+
+namespace hydra {
+namespace rope {
+
+constexpr int kMostAxes = 4;
+constexpr int kWaves = 4;      // of a workgroup
+constexpr int kRowsInFlight = 4;  // rows that a lane has loaded before it computes
+
+struct Args {
+  const uint16_t *q, *k, *v;
+  uint16_t *q_out, *k_out;
+  uint16_t *k_cache, *v_cache;
+  int64_t q_stride, k_stride, v_stride, q_out_stride, k_out_stride;  // elements per token
+  const uint16_t *q_weight, *k_weight;
+  const int32_t* positions;
+  int64_t axis_stride;
+  const float* inv_freq;
+  const int32_t* freq_axis;
+  const int64_t* slot_mapping;
+  int64_t num_slots;
+  float eps;
+  int32_t n_axes, rotary_pieces, interleaved;  // rotary_pieces: 16-byte pieces of half of the rotated part
+  int32_t total_tokens, n_q_heads, n_kv_heads, n_rows;  // n_rows: q's, k's and, with a cache, v's
+  int32_t parts, rows_per_part;                // waves per token
+};
+
+// Lanes per row.  With a norm they are the lanes that sum_over_row knows: a power of two, three of eight idle at head_dim 80.
+template <int D, bool NORM>
+constexpr int kRowLanes = D == 80 ? (NORM ? 8 : 5) : D / 16;
+template <int D, bool NORM>
+constexpr int kRowsPerWave = 64 / kRowLanes<D, NORM>;
+
+#if defined(__HIP_DEVICE_COMPILE__)
+
+// Sum over the 4 or 8 neighbouring lanes of a row, in all of them.
+template <int LANES>
+__device__ __forceinline__ float sum_over_row(float x) {
+  auto add = [&](auto ctrl) { x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xf, 0xf, true)); };
+  add(std::integral_constant<int, 0xB1>{});  // lanes 1 0 3 2
+  add(std::integral_constant<int, 0x4E>{});  // lanes 2 3 0 1
+  if constexpr (LANES == 8) add(std::integral_constant<int, 0x141>{});  // the other four of eight (mirrored)
+  return x;
+}
+
+__device__ __forceinline__ float low_half(uint32_t x) { return __builtin_bit_cast(float, x << 16); }
+__device__ __forceinline__ float high_half(uint32_t x) { return __builtin_bit_cast(float, x & 0xffff0000u); }
+
+__device__ __forceinline__ void unpack(const u32x4_t& piece, float (&x)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = low_half(piece[i]);
+    x[2 * i + 1] = high_half(piece[i]);
+  }
+}
+__device__ __forceinline__ u32x4_t pack(const float (&x)[8]) {
+  u32x4_t piece;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const f32x2_t two = {x[2 * i], x[2 * i + 1]};
+    piece[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(two, bf16x2_t));
+  }
+  return piece;
+}
+
+#endif  // __HIP_DEVICE_COMPILE__
+
+// grid: a wave per part of a token
+template <int D, bool NORM>
+__global__ __launch_bounds__(64 * kWaves) void qk_norm_rope_kernel(const Args a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  constexpr int LANES = kRowLanes<D, NORM>, PIECES = D / 16, ROWS = kRowsPerWave<D, NORM>;
+  const int lane = (int)threadIdx.x & 63;
+  const int64_t unit = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int token = (int)(unit / a.parts), part = (int)(unit - (int64_t)token * a.parts);
+  if (token >= a.total_tokens) return;
+  const int lane_row = lane / LANES, piece = lane - lane_row * LANES;
+  const bool active = lane_row < ROWS && piece < PIECES;
+
+  // this lane's pieces of a row: l and u hold the lower and the upper elements of rotated pairs, or elements that stay
+  const int rp = a.rotary_pieces;
+  const bool rotates = piece < rp;
+  const int l = rotates ? piece : 2 * rp + (piece - rp), u = rotates ? piece + rp : PIECES + piece;
+  float w_q[16], w_k[16];
+  if constexpr (NORM) {
+    const u32x4_t ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+    auto weights = [&](const uint16_t* w, float (&to)[16]) {
+      const bool there = active && w != nullptr;
+      const u32x4_t wl = there ? reinterpret_cast<const u32x4_t*>(w)[l] : ones, wu = there ? reinterpret_cast<const u32x4_t*>(w)[u] : ones;
+      float x[8];
+      unpack(wl, x);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) to[i] = x[i];
+      unpack(wu, x);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) to[8 + i] = x[i];
+    };
+    weights(a.q_weight, w_q);
+    weights(a.k_weight, w_k);
+  }
+
+  const int64_t slot = a.k_cache ? a.slot_mapping[token] : -1;
+  const bool cached = slot >= 0 && slot < a.num_slots;
+  const int row_end = (part + 1) * a.rows_per_part < a.n_rows ? (part + 1) * a.rows_per_part : a.n_rows;
+  const uint16_t* q_in = a.q + (int64_t)token * a.q_stride;
+  const uint16_t* k_in = a.k + (int64_t)token * a.k_stride;
+  const uint16_t* v_in = a.v + (int64_t)token * a.v_stride;
+  const int k_first = a.n_q_heads, v_first = a.n_q_heads + a.n_kv_heads;
+
+  float cosine[8], sine[8];
+  bool have_angles = false;
+  for (int row0 = part * a.rows_per_part; row0 < row_end; row0 += ROWS * kRowsInFlight) {
+    u32x4_t low[kRowsInFlight], up[kRowsInFlight];
+    auto row_of = [&](int i) { return row0 + i * ROWS + lane_row; };
+#pragma unroll
+    for (int i = 0; i < kRowsInFlight; ++i) {
+      const int row = row_of(i);
+      if (active && row < row_end) {
+        const uint16_t* from = row < k_first ? q_in + (int64_t)row * D : row < v_first ? k_in + (int64_t)(row - k_first) * D : v_in + (int64_t)(row - v_first) * D;
+        low[i] = reinterpret_cast<const u32x4_t*>(from)[l];
+        up[i] = reinterpret_cast<const u32x4_t*>(from)[u];
+      }
+    }
+    if (!have_angles) {
+      have_angles = true;
+      if (active && rotates) {
+        int32_t at[kMostAxes];
+#pragma unroll
+        for (int x = 0; x < kMostAxes; ++x) at[x] = a.positions[(int64_t)(x < a.n_axes ? x : 0) * a.axis_stride + token];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int pair = a.interleaved ? (i < 4 ? 4 * l + i : 4 * u + i - 4) : 8 * l + i;
+          int axis = a.freq_axis ? a.freq_axis[pair] : 0;
+          axis = axis < 0 ? 0 : (axis >= a.n_axes ? a.n_axes - 1 : axis);
+          const int32_t position = axis == 0 ? at[0] : axis == 1 ? at[1] : axis == 2 ? at[2] : at[3];
+          double part_of_turn = (double)a.inv_freq[pair] * 0.15915494309189533577;  // 1 / (2 pi)
+          part_of_turn -= __builtin_rint(part_of_turn);
+          const uint64_t per_position = (uint64_t)(int64_t)(part_of_turn * 0x1p62) * 4;  // (modulo whole turns)
+          const int32_t phase = (int32_t)(((uint64_t)(int64_t)position * per_position) >> 32);
+          const float turns = (float)phase * 0x1p-32f;
+          cosine[i] = __builtin_amdgcn_cosf(turns);
+          sine[i] = __builtin_amdgcn_sinf(turns);
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kRowsInFlight; ++i) {
+      const int row = row_of(i);
+      const bool there = active && row < row_end, is_v = row >= v_first;
+      float x[8], y[8];
+      unpack(low[i], x);
+      unpack(up[i], y);
+      if constexpr (NORM) {
+        float squares = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          squares = __builtin_fmaf(x[j], x[j], squares);
+          squares = __builtin_fmaf(y[j], y[j], squares);
+        }
+        squares = sum_over_row<LANES>(there ? squares : 0.f);
+        const bool is_q = row < k_first;
+        const bool normed = is_q ? a.q_weight != nullptr : a.k_weight != nullptr;
+        const float scale = normed ? 1.0f / __builtin_sqrtf(squares * (1.0f / D) + a.eps) : 1.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          x[j] = x[j] * scale * (is_q ? w_q[j] : w_k[j]);
+          y[j] = y[j] * scale * (is_q ? w_q[8 + j] : w_k[8 + j]);
+        }
+      }
+      float xr[8], yr[8];
+      if (!rotates) {  // (as they are: no product with a sine of 0, which an infinity beside them would turn into NaN)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          xr[j] = x[j];
+          yr[j] = y[j];
+        }
+      } else if (a.interleaved) {
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+          const int e = j / 2;
+          xr[j] = x[j] * cosine[e] - x[j + 1] * sine[e];
+          xr[j + 1] = x[j + 1] * cosine[e] + x[j] * sine[e];
+          yr[j] = y[j] * cosine[4 + e] - y[j + 1] * sine[4 + e];
+          yr[j + 1] = y[j + 1] * cosine[4 + e] + y[j] * sine[4 + e];
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          xr[j] = x[j] * cosine[j] - y[j] * sine[j];
+          yr[j] = y[j] * cosine[j] + x[j] * sine[j];
+        }
+      }
+      if (!there) continue;
+      const u32x4_t low_out = is_v ? low[i] : pack(xr), up_out = is_v ? up[i] : pack(yr);
+      if (row < k_first) {
+        u32x4_t* to = reinterpret_cast<u32x4_t*>(a.q_out + (int64_t)token * a.q_out_stride + (int64_t)row * D);
+        to[l] = low_out;
+        to[u] = up_out;
+        continue;
+      }
+      const int head = is_v ? row - v_first : row - k_first;
+      if (!is_v && a.k_out) {
+        u32x4_t* to = reinterpret_cast<u32x4_t*>(a.k_out + (int64_t)token * a.k_out_stride + (int64_t)head * D);
+        to[l] = low_out;
+        to[u] = up_out;
+      }
+      if (cached) {
+        u32x4_t* to = reinterpret_cast<u32x4_t*>((is_v ? a.v_cache : a.k_cache) + (slot * a.n_kv_heads + head) * D);
+        to[l] = low_out;
+        to[u] = up_out;
+      }
+    }
+  }
+#else
+  (void)a;
+#endif
+}
+
+}  // namespace rope
+}  // namespace hydra

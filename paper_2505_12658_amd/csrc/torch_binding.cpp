@@ -1,4 +1,4 @@
-// Python binding of include/hydra_attn.h for torch tensors: checks, data pointers, strides and the
+// Python binding of include/hydra_attn.h and include/hydra_step.h for torch tensors: checks, data pointers, strides and the
 // current stream, then one call through the C ABI.  Every step of the computation runs in the HIP kernels.
 //
 // The marshalling is native because a decode step or a single image is over in tens of microseconds: written
@@ -11,13 +11,16 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <dlfcn.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <exception>
+#include <initializer_list>
 
 #include "../../include/hydra_attn.h"
+#include "../../include/hydra_step.h"
 
 namespace {
 
@@ -33,6 +36,8 @@ struct Library {
   decltype(&hydra_attn_paged_workspace_bytes) attn_paged_workspace_bytes = nullptr;
   decltype(&hydra_page_cache_write) page_cache_write = nullptr;
   decltype(&hydra_page_cache_gather) page_cache_gather = nullptr;
+  decltype(&hydra_page_maps_build) page_maps_build = nullptr;
+  decltype(&hydra_qk_norm_rope) qk_norm_rope = nullptr;
 };
 Library lib;
 PyObject* hydra_error = nullptr;  // the HydraError class: HydraError(status, where)
@@ -333,6 +338,144 @@ PyObject* py_page_cache_gather(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ---- include/hydra_step.h ----
+// These calls run on the device of their tensors, whichever is current, and refuse tensors of several devices.
+
+// a tensor, or nullptr for None
+const at::Tensor* maybe(PyObject* o, const char* name) { return o == Py_None ? nullptr : &tensor(o, name); }
+const at::Tensor* maybe_index(PyObject* o, at::ScalarType type, const char* name) { return o == Py_None ? nullptr : &index_array(o, type, name); }
+
+void same_device(const at::Tensor& with, std::initializer_list<const at::Tensor*> others) {
+  for (const at::Tensor* t : others)
+    if (t && t->device() != with.device()) raise(PyExc_ValueError, "all tensors must be on one device");
+}
+// The stream of a call on `device`, which is current: the one given, or the device's current one.
+void* stream_on(PyObject* o, c10::Device device) {
+  if (o == Py_None) return c10::hip::getCurrentHIPStream(device.index()).stream();
+  PyObject* index = PyObject_GetAttrString(o, "device_index");
+  if (!index) throw Raised{};
+  const long of = PyLong_AsLong(index);
+  Py_DECREF(index);
+  if (of == -1 && PyErr_Occurred()) throw Raised{};
+  if (of != device.index()) raise(PyExc_ValueError, "stream must belong to the tensors' device");
+  return stream_handle(o);
+}
+// Memory that the call allocated itself and uses on a stream that was given: not handed out again before that stream is through.
+void used_on(PyObject* o, const at::Tensor& t) {
+  if (o == Py_None || !t.defined()) return;
+  int64_t field[3];
+  const char* const names[3] = {"stream_id", "device_index", "device_type"};
+  for (int i = 0; i < 3; ++i) {
+    PyObject* v = PyObject_GetAttrString(o, names[i]);
+    if (!v) throw Raised{};
+    field[i] = PyLong_AsLongLong(v);
+    Py_DECREF(v);
+    if (field[i] == -1 && PyErr_Occurred()) throw Raised{};
+  }
+  t.record_stream(c10::Stream::unpack3(field[0], (c10::DeviceIndex)field[1], (c10::DeviceType)field[2]));
+}
+template <typename T>
+T* data(const at::Tensor* t) { return t ? static_cast<T*>(t->data_ptr()) : nullptr; }
+
+// q_lens, context_lens, block_tables, free_blocks, n_free, total_tokens, block_size, num_blocks, position_deltas,
+// the six outputs (positions and next_context may be None), stream
+PyObject* py_page_maps_build(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded("page_maps_build", n, 16, [&] {
+    const at::Tensor &q = index_array(a[0], at::kInt, "q_lens"), &context = index_array(a[1], at::kInt, "context_lens"), &table = index_array(a[2], at::kInt, "block_tables"),
+                     &list = index_array(a[3], at::kInt, "free_blocks"), &n_free = index_array(a[4], at::kInt, "n_free");
+    const at::Tensor* deltas = maybe_index(a[8], at::kInt, "position_deltas");
+    const at::Tensor &cu = index_array(a[9], at::kInt, "cu_seqlens_q"), &kv = index_array(a[10], at::kInt, "kv_lens"), &slots = index_array(a[11], at::kLong, "slot_mapping");
+    const at::Tensor *positions = maybe_index(a[12], at::kInt, "positions"), *next = maybe_index(a[13], at::kInt, "next_context");
+    const at::Tensor& pool = index_array(a[14], at::kInt, "pool");
+    same_device(q, {&context, &table, &list, &n_free, deltas, &cu, &kv, &slots, positions, next, &pool});
+    const int64_t batch = q.numel();
+    const int32_t total = whole(a[5]), block = whole(a[6]);
+    const int64_t blocks = PyLong_AsLongLong(a[7]);
+    if (blocks == -1 && PyErr_Occurred()) throw Raised{};
+    if (context.numel() != batch || table.dim() != 2 || table.size(0) != batch || n_free.numel() < 1 || (deltas && deltas->numel() != batch) || cu.numel() != batch + 1 ||
+        kv.numel() != batch || slots.numel() < total || (positions && positions->numel() < total) || (next && next->numel() != batch) || pool.numel() < 2)
+      raise(PyExc_ValueError, "shape mismatch between q_lens, context_lens, block_tables and the maps");
+    const int32_t width = size32(table.size(1)), capacity = size32(list.numel()), rows = size32(batch);
+    const c10::OptionalDeviceGuard guard(q.device());
+    void* s = stream_on(a[15], q.device());
+    call("hydra_page_maps_build", [&] {
+      return lib.page_maps_build(data<int32_t>(&q), data<int32_t>(&context), data<int32_t>(&table), width, data<int32_t>(&list), capacity, data<int32_t>(&n_free),
+                                 data<int32_t>(deltas), rows, total, block, blocks, data<int32_t>(&cu), data<int32_t>(&kv), data<int64_t>(&slots), data<int32_t>(positions),
+                                 data<int32_t>(next), data<int32_t>(&pool), s);
+    });
+    return Py_NewRef(Py_None);
+  });
+}
+
+const at::Tensor* head_weight(PyObject* o, int64_t d, const char* name) {
+  const at::Tensor* t = maybe(o, name);
+  if (t && (!is_bf16(*t) || !t->is_cuda() || !t->is_contiguous() || t->numel() != d)) raise(PyExc_TypeError, name, " must be a contiguous CUDA bf16 tensor [head_dim]");
+  return t;
+}
+
+// q, k, positions, inv_freq, freq_axis, q_weight, k_weight, eps, interleaved, q_out, k_out, v, k_cache, v_cache, slot_mapping, stream
+PyObject* py_qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded("qk_norm_rope", n, 16, [&] {
+    const at::Tensor &q = token_major(a[0], "q"), &k = token_major(a[1], "k");
+    const int64_t tokens = q.size(0), d = q.size(2);
+    if (k.size(0) != tokens || k.size(2) != d) raise(PyExc_ValueError, "q and k must have the same tokens and head_dim");
+    const at::Tensor *positions = maybe(a[2], "positions"), *freq = maybe(a[3], "inv_freq"), *axis = maybe_index(a[4], at::kInt, "freq_axis");
+    if (freq && (freq->scalar_type() != at::kFloat || !freq->is_cuda() || !freq->is_contiguous() || freq->dim() != 1)) raise(PyExc_TypeError, "inv_freq must be a contiguous CUDA fp32 vector");
+    if (axis && (!freq || axis->numel() != freq->numel())) raise(PyExc_ValueError, "freq_axis must have one entry per frequency");
+    const bool rotates = freq && freq->numel() > 0;
+    if (rotates) {
+      if (!positions) raise(PyExc_ValueError, "positions are needed for a rotation");
+      if (positions->scalar_type() != at::kInt || !positions->is_cuda() || positions->dim() < 1 || positions->dim() > 2)
+        raise(PyExc_TypeError, "positions must be a CUDA int32 tensor [tokens] or [axes, tokens]");
+      if (positions->size(-1) != tokens || (tokens > 1 && positions->stride(-1) != 1) || (positions->dim() == 2 && positions->size(0) < 1))
+        raise(PyExc_ValueError, "positions must have one entry per token, next to each other, on at least one axis");
+    }
+    const at::Tensor *q_weight = head_weight(a[5], d, "q_weight"), *k_weight = head_weight(a[6], d, "k_weight");
+    const float eps = (float)real(a[7]);
+    const int interleaved = truth(a[8]);
+    const at::Tensor *v = a[11] == Py_None ? nullptr : &token_major(a[11], "v"), *kc = maybe(a[12], "k_cache"), *vc = maybe(a[13], "v_cache"),
+                     *slots = maybe_index(a[14], at::kLong, "slot_mapping");
+    const bool cached = kc || vc || slots;
+    if (cached) {
+      if (!v || !kc || !vc || !slots) raise(PyExc_ValueError, "v, k_cache, v_cache and slot_mapping go together");
+      check_caches(*kc, *vc);
+      if (v->sizes() != k.sizes() || slots->numel() != tokens || kc->size(2) != k.size(1) || kc->size(3) != d) raise(PyExc_ValueError, "shape mismatch between k/v, caches and slot_mapping");
+    }
+    same_device(q, {&k, rotates ? positions : nullptr, freq, axis, q_weight, k_weight, v, kc, vc, slots});
+    const c10::OptionalDeviceGuard guard(q.device());
+    auto output = [&](PyObject* o, const at::Tensor& like, const char* name) {
+      if (o == Py_None) {
+        at::Tensor t = at::empty(like.sizes(), like.options().memory_format(c10::nullopt));
+        used_on(a[15], t);
+        return t;
+      }
+      const at::Tensor& t = token_major(o, name);
+      if (t.sizes() != like.sizes()) raise(PyExc_ValueError, name, " must be shaped like its input");
+      same_device(q, {&t});
+      return t;
+    };
+    const at::Tensor q_out = output(a[9], q, "q_out");
+    at::Tensor k_out;
+    if (a[10] != Py_None || !cached) k_out = output(a[10], k, "k_out");
+    const int32_t n_axes = rotates && positions->dim() == 2 ? size32(positions->size(0)) : 1;
+    const int64_t axis_stride = rotates && positions->dim() == 2 ? positions->stride(0) : 0;
+    const int32_t rotary = rotates ? size32(2 * freq->numel()) : 0, total = size32(tokens), hq = size32(q.size(1)), hkv = size32(k.size(1)), dim = size32(d);
+    const int32_t block = cached ? size32(kc->size(1)) : 1;
+    void* s = stream_on(a[15], q.device());
+    call("hydra_qk_norm_rope", [&] {
+      return lib.qk_norm_rope(q.data_ptr(), k.data_ptr(), cached ? v->data_ptr() : nullptr, q.stride(0), k.stride(0), cached ? v->stride(0) : 0, q_out.data_ptr(),
+                              k_out.defined() ? k_out.data_ptr() : nullptr, q_out.stride(0), k_out.defined() ? k_out.stride(0) : 0, data<void>(q_weight), data<void>(k_weight), eps,
+                              rotates ? data<int32_t>(positions) : nullptr, axis_stride, n_axes, rotates ? data<float>(freq) : nullptr, data<int32_t>(axis), rotary, interleaved,
+                              data<void>(kc), data<void>(vc), data<int64_t>(slots), block, cached ? kc->size(0) : 0, total, hq, hkv, dim, s);
+    });
+    PyObject *first = THPVariable_Wrap(q_out), *second = k_out.defined() ? THPVariable_Wrap(k_out) : Py_NewRef(Py_None);
+    PyObject* both = first && second ? PyTuple_Pack(2, first, second) : nullptr;
+    Py_XDECREF(first);
+    Py_XDECREF(second);
+    return both;
+  });
+}
+
 // load(path, HydraError): opens the library and looks its entry points up
 PyObject* py_load(PyObject*, PyObject* args) {
   const char* path;
@@ -360,8 +503,10 @@ PyObject* py_load(PyObject*, PyObject* args) {
   find(l.attn_paged_workspace_bytes, "hydra_attn_paged_workspace_bytes");
   find(l.page_cache_write, "hydra_page_cache_write");
   find(l.page_cache_gather, "hydra_page_cache_gather");
+  find(l.page_maps_build, "hydra_page_maps_build");
+  find(l.qk_norm_rope, "hydra_qk_norm_rope");
   if (!all) {
-    PyErr_Format(PyExc_ImportError, "%s lacks an entry point of hydra_attn.h", path);
+    PyErr_Format(PyExc_ImportError, "%s lacks an entry point of hydra_attn.h or hydra_step.h", path);
     return nullptr;
   }
   lib = l;
@@ -381,6 +526,8 @@ PyMethodDef methods[] = {{"load", py_load, METH_VARARGS, nullptr},
                          HYDRA_FAST(attn_paged_fwd),
                          HYDRA_FAST(page_cache_write),
                          HYDRA_FAST(page_cache_gather),
+                         HYDRA_FAST(page_maps_build),
+                         HYDRA_FAST(qk_norm_rope),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_hydra_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
