@@ -5,6 +5,8 @@
  *                           free list, block tables, cache slots, positions, packed offsets, context lengths
  *   hydra_qk_norm_rope      queries and keys of one layer: norm of every head, rotation by positions with one or several axes
  *                           (time, height, width), and K and V into the paged cache, in one pass
+ *   hydra_attn_prefix_fwd   attention over the paged cache of requests in groups whose contexts begin with the same cached tokens, which
+ *                           are read once for all of a group's queries
  *
  * The arrays are those of hydra_attn.h: bf16 tokens [tokens, heads, head_dim] with a token stride, int32 lengths and tables, int64
  * slots, caches [num_blocks, block_size, n_kv_heads, head_dim].  So are the conventions: device pointers owned by the caller, work
@@ -99,6 +101,52 @@ int hydra_qk_norm_rope(const void* q, const void* k, const void* v, int64_t q_to
                        const float* inv_freq, const int32_t* freq_axis, int32_t rotary_dim, int32_t interleaved,
                        void* k_cache, void* v_cache, const int64_t* slot_mapping, int32_t block_size, int64_t num_blocks,
                        int32_t total_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, void* stream);
+
+/*
+ * Attention over the paged cache of requests that share prefixes.
+ *
+ * hydra_attn_paged_fwd for a batch in groups: requests cu_groups[g] .. cu_groups[g + 1] - 1, next to each other, begin with the same
+ * shared_lens[g] tokens, whose keys and values lie in the same cache blocks (the same instructions, examples, image or document; several answers
+ * to one prompt).  Arguments and results are those of hydra_attn_paged_fwd, to rounding: request b's row of block_tables names all of its
+ * blocks, the shared ones first, and kv_lens[b] counts all of its context.  What the groups say is only where keys may be read once for all of a
+ * group's new tokens, instead of once per request:
+ *
+ *   cu_groups     device int32 [n_groups + 1]; cu_groups[0] == 0, non-decreasing, cu_groups[n_groups] == batch.
+ *   shared_lens   device int32 [n_groups], 0 or less: nothing is shared.  The first shared_lens[g] keys of all of the group's requests that have new
+ *        tokens have to be the same; the kernels find them by the row of block_tables of the first such request.  Of a number that is larger
+ *        than a token of the group can see (kv_len - q_len + 1), and of one that is no multiple of 64, less is used; and nothing where
+ *        it would not pay.
+ *   q, out, k_cache, v_cache, block_tables, cu_seqlens_q, kv_lens, softmax_scale, head_dim, block_size, num_blocks  as for
+ *        hydra_attn_paged_fwd.  A request with q_len == 0 (or, invalidly, kv_len < q_len) produces no output, and its rows of out are left as they
+ *        were.  The keys and values of the contexts are finite.
+ *   batch and n_groups at most 2048, total_q * n_q_heads at most 2^24.
+ *   workspace     device memory, 16-byte aligned, at least hydra_attn_prefix_workspace_bytes(...) bytes.  It need not be initialised and may be
+ *        reused by the next call on the same stream.
+ *
+ * The call is made of two halves, for callers that run many layers over one batch: hydra_attn_prefix_plan reads the lengths and
+ * writes the plan into the workspace, and hydra_attn_prefix_fwd_planned runs one layer's attention by it, any number of times, on the same
+ * stream, with the SAME batch, n_groups, total_q, head counts, head_dim, max_blocks_per_seq and block_size.  Two calls that share a workspace must not
+ * overlap in time, recorded in graphs or not.
+ *
+ * batch == 0 or total_q == 0 returns HYDRA_OK without launching.
+ */
+int hydra_attn_prefix_fwd(const void* q, void* out, int64_t q_token_stride, const void* k_cache, const void* v_cache, const int32_t* block_tables,
+                          int32_t max_blocks_per_seq, const int32_t* cu_seqlens_q, const int32_t* kv_lens, const int32_t* cu_groups,
+                          const int32_t* shared_lens, int32_t batch, int32_t n_groups, int32_t total_q, int32_t n_q_heads, int32_t n_kv_heads,
+                          int32_t head_dim, int32_t block_size, int64_t num_blocks, float softmax_scale, void* workspace, size_t workspace_bytes,
+                          void* stream);
+
+int hydra_attn_prefix_plan(const int32_t* cu_seqlens_q, const int32_t* kv_lens, const int32_t* cu_groups, const int32_t* shared_lens,
+                           int32_t batch, int32_t n_groups, int32_t total_q, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                           int32_t max_blocks_per_seq, int32_t block_size, void* workspace, size_t workspace_bytes, void* stream);
+
+int hydra_attn_prefix_fwd_planned(const void* q, void* out, int64_t q_token_stride, const void* k_cache, const void* v_cache,
+                                  const int32_t* block_tables, int32_t max_blocks_per_seq, int32_t batch, int32_t n_groups, int32_t total_q,
+                                  int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t block_size, int64_t num_blocks,
+                                  float softmax_scale, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace for these sizes (0 if they are invalid or unsupported).  Pure host arithmetic. */
+size_t hydra_attn_prefix_workspace_bytes(int32_t batch, int32_t n_groups, int32_t total_q, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim);
 
 #ifdef __cplusplus
 }

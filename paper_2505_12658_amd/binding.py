@@ -66,6 +66,14 @@ def load_library() -> ctypes.CDLL:
         lib.hydra_qk_norm_rope.restype = ctypes.c_int
         lib.hydra_qk_norm_rope.argtypes = [vp, vp, vp, i64, i64, i64, vp, vp, i64, i64, vp, vp, ctypes.c_float, vp, i64, i32, vp, vp, i32, i32, vp, vp, vp, i32, i64,
                                            i32, i32, i32, i32, vp]
+        lib.hydra_attn_prefix_workspace_bytes.restype = sz
+        lib.hydra_attn_prefix_workspace_bytes.argtypes = [i32] * 6
+        lib.hydra_attn_prefix_plan.restype = ctypes.c_int
+        lib.hydra_attn_prefix_plan.argtypes = [vp, vp, vp, vp] + [i32] * 8 + [vp, sz, vp]
+        lib.hydra_attn_prefix_fwd.restype = ctypes.c_int
+        lib.hydra_attn_prefix_fwd.argtypes = [vp, vp, i64, vp, vp, vp, i32, vp, vp, vp, vp] + [i32] * 7 + [i64, ctypes.c_float, vp, sz, vp]
+        lib.hydra_attn_prefix_fwd_planned.restype = ctypes.c_int
+        lib.hydra_attn_prefix_fwd_planned.argtypes = [vp, vp, i64, vp, vp, vp, i32] + [i32] * 7 + [i64, ctypes.c_float, vp, sz, vp]
         lib.hydra_attn_workspace_bytes.restype = sz
         lib.hydra_attn_workspace_bytes.argtypes = [i32] * 6
         lib.hydra_status_string.restype = ctypes.c_char_p
@@ -200,3 +208,30 @@ def hydra_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: Optional[tor
     themselves for in place), or new ones.  With caches [num_blocks, block_size, Hkv, d] the rows of k, and v's as they are, go to slot_mapping (int64 [N], < 0 skips)
     there, and to k_out only if it is given (None is returned otherwise)."""
     return _calls().qk_norm_rope(q, k, positions, inv_freq, freq_axis, q_weight, k_weight, eps, interleaved, q_out, k_out, v, k_cache, v_cache, slot_mapping, stream)
+
+
+def hydra_attn_prefix_workspace_bytes(batch: int, n_groups: int, total_q: int, n_q_heads: int, n_kv_heads: int, head_dim: int) -> int:
+    return int(load_library().hydra_attn_prefix_workspace_bytes(batch, n_groups, total_q, n_q_heads, n_kv_heads, head_dim))
+
+
+def hydra_attn_prefix_fwd(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, block_tables: torch.Tensor, cu_seqlens_q: torch.Tensor,
+                          kv_lens: torch.Tensor, cu_groups: torch.Tensor, shared_lens: torch.Tensor, softmax_scale: float,
+                          out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                          stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """hydra_attn_paged_fwd for requests in groups: requests cu_groups[g] .. cu_groups[g + 1] - 1 (int32 [G + 1]) begin with the same shared_lens[g]
+    (int32 [G]) cached tokens, in the same blocks, which are read once for all of them.  workspace: uint8 tensor of
+    hydra_attn_prefix_workspace_bytes(...) (allocated if None)."""
+    return _calls().attn_prefix_fwd(q, k_cache, v_cache, block_tables, cu_seqlens_q, kv_lens, cu_groups, shared_lens, softmax_scale, out, workspace, stream)
+
+
+def hydra_attn_prefix_plan(cu_seqlens_q: torch.Tensor, kv_lens: torch.Tensor, cu_groups: torch.Tensor, shared_lens: torch.Tensor, total_q: int,
+                           n_q_heads: int, n_kv_heads: int, head_dim: int, max_blocks_per_seq: int, block_size: int,
+                           workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """The plan of one batch, for hydra_attn_prefix_fwd_planned in every layer; returns the workspace that holds it (allocated if None)."""
+    return _calls().attn_prefix_plan(cu_seqlens_q, kv_lens, cu_groups, shared_lens, total_q, n_q_heads, n_kv_heads, head_dim, max_blocks_per_seq, block_size, workspace, stream)
+
+
+def hydra_attn_prefix_fwd_planned(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, block_tables: torch.Tensor, n_groups: int, softmax_scale: float,
+                                  workspace: torch.Tensor, out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """hydra_attn_prefix_fwd of a batch that hydra_attn_prefix_plan has planned into `workspace`."""
+    return _calls().attn_prefix_fwd_planned(q, k_cache, v_cache, block_tables, n_groups, softmax_scale, workspace, out, stream)

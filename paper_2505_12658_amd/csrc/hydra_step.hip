@@ -4,8 +4,10 @@
 #include <stdint.h>
 
 #include "../../include/hydra_step.h"
+#include "attn_prefix.hpp"
 #include "launch.hpp"
 #include "page_maps.hpp"
+#include "prefix_plan.hpp"
 #include "qk_rope.hpp"
 
 using hydra::aligned16, hydra::head_dim_supported, hydra::launch;
@@ -157,6 +159,161 @@ int hydra_qk_norm_rope(const void* q, const void* k, const void* v, int64_t q_to
   };
   const hipError_t err = q_weight || k_weight ? launch_dim(bool_constant<true>{}) : launch_dim(bool_constant<false>{});
   return err == hipSuccess ? HYDRA_OK : HYDRA_ERR_LAUNCH;
+}
+
+}  // extern "C"
+
+namespace {
+
+namespace prefix = hydra::prefix;
+
+// What the three calls of attention over shared prefixes check alike.
+int check_prefix_sizes(int32_t batch, int32_t n_groups, int32_t total_q, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim) {
+  if (batch < 0 || n_groups < 0 || total_q < 0 || n_q_heads <= 0 || n_kv_heads <= 0 || n_q_heads % n_kv_heads != 0) return HYDRA_ERR_INVALID_ARG;
+  if (!head_dim_supported(head_dim) || batch > prefix::kMostRequests || n_groups > prefix::kMostRequests) return HYDRA_ERR_UNSUPPORTED;
+  if (batch > 0 && total_q > 0 && n_groups < 1) return HYDRA_ERR_INVALID_ARG;
+  if ((int64_t)total_q * n_q_heads > (int64_t)1 << 24) return HYDRA_ERR_UNSUPPORTED;
+  // (a workgroup of 256 threads per piece and KV head)
+  if (prefix::layout_of(batch, n_groups, total_q, n_q_heads / n_kv_heads, n_kv_heads, head_dim).pieces * n_kv_heads > 0x7fffff) return HYDRA_ERR_UNSUPPORTED;
+  return HYDRA_OK;
+}
+int check_prefix_workspace(const void* workspace, size_t workspace_bytes, const prefix::Layout& layout) {
+  return !workspace || !aligned16(workspace) || workspace_bytes < layout.total ? HYDRA_ERR_WORKSPACE : HYDRA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t hydra_attn_prefix_workspace_bytes(int32_t batch, int32_t n_groups, int32_t total_q, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim) {
+  if (check_prefix_sizes(batch, n_groups, total_q, n_q_heads, n_kv_heads, head_dim) != HYDRA_OK) return 0;
+  return prefix::layout_of(batch, n_groups, total_q, n_q_heads / n_kv_heads, n_kv_heads, head_dim).total;
+}
+
+int hydra_attn_prefix_plan(const int32_t* cu_seqlens_q, const int32_t* kv_lens, const int32_t* cu_groups, const int32_t* shared_lens,
+                           int32_t batch, int32_t n_groups, int32_t total_q, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                           int32_t max_blocks_per_seq, int32_t block_size, void* workspace, size_t workspace_bytes, void* stream) {
+  if (int rc = check_prefix_sizes(batch, n_groups, total_q, n_q_heads, n_kv_heads, head_dim)) return rc;
+  if (max_blocks_per_seq < 1 || block_size < 1) return batch == 0 || total_q == 0 ? HYDRA_OK : HYDRA_ERR_INVALID_ARG;
+  if (block_shift_of(block_size, 0, max_blocks_per_seq) < 0) return HYDRA_ERR_UNSUPPORTED;
+  if (batch == 0 || total_q == 0) return HYDRA_OK;
+  if (!cu_seqlens_q || !kv_lens || !cu_groups || !shared_lens) return HYDRA_ERR_INVALID_ARG;
+  const prefix::Layout layout = prefix::layout_of(batch, n_groups, total_q, n_q_heads / n_kv_heads, n_kv_heads, head_dim);
+  if (int rc = check_prefix_workspace(workspace, workspace_bytes, layout)) return rc;
+
+  unsigned char* const ws = static_cast<unsigned char*>(workspace);
+  prefix::PlanArgs args;
+  args.cu_seqlens_q = cu_seqlens_q;
+  args.kv_lens = kv_lens;
+  args.cu_groups = cu_groups;
+  args.shared_lens = shared_lens;
+  args.header = reinterpret_cast<prefix::PlanHeader*>(ws);
+  args.pieces = reinterpret_cast<prefix::Piece*>(ws + layout.pieces_at);
+  args.tokens = reinterpret_cast<prefix::Token*>(ws + layout.tokens_at);
+  args.batch = batch;
+  args.n_groups = n_groups;
+  args.total_q = total_q;
+  args.group = n_q_heads / n_kv_heads;
+  args.n_kv_heads = n_kv_heads;
+  args.table_keys = max_blocks_per_seq * block_size;
+  args.pieces_capacity = (int32_t)layout.pieces;
+  args.rows_capacity = (int32_t)layout.rows;
+  const hipError_t err = hydra::launch_lds(prefix::prefix_plan_kernel, dim3(1), dim3(prefix::kPlanThreads), prefix::plan_lds_bytes(batch, n_groups),
+                                           static_cast<hipStream_t>(stream), args);
+  return err == hipSuccess ? HYDRA_OK : HYDRA_ERR_LAUNCH;
+}
+
+namespace {
+
+// Every argument of the attention call but the plan's lengths; *done: there is nothing to do.
+int check_prefix_call(const void* q, const void* out, int64_t q_token_stride, const void* k_cache, const void* v_cache, const int32_t* block_tables,
+                      int32_t max_blocks_per_seq, int32_t batch, int32_t n_groups, int32_t total_q, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                      int32_t block_size, int64_t num_blocks, float softmax_scale, const void* workspace, size_t workspace_bytes, bool* done) {
+  *done = false;
+  if (int rc = check_prefix_sizes(batch, n_groups, total_q, n_q_heads, n_kv_heads, head_dim)) return rc;
+  if (block_size < 1 || (block_size & (block_size - 1)) != 0) return HYDRA_ERR_UNSUPPORTED;
+  if (!(softmax_scale >= 0.0f) || isinf(softmax_scale)) return HYDRA_ERR_INVALID_ARG;
+  if (batch == 0 || total_q == 0) {
+    *done = true;
+    return HYDRA_OK;
+  }
+  if (max_blocks_per_seq < 1 || num_blocks < 1) return HYDRA_ERR_INVALID_ARG;
+  if (!q || !out || !k_cache || !v_cache || !block_tables) return HYDRA_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(out) || !aligned16(k_cache) || !aligned16(v_cache)) return HYDRA_ERR_INVALID_ARG;
+  if (q_token_stride < (int64_t)n_q_heads * head_dim || (q_token_stride & 7)) return HYDRA_ERR_INVALID_ARG;
+  if (block_shift_of(block_size, num_blocks, max_blocks_per_seq) < 0) return HYDRA_ERR_UNSUPPORTED;
+  return check_prefix_workspace(workspace, workspace_bytes, prefix::layout_of(batch, n_groups, total_q, n_q_heads / n_kv_heads, n_kv_heads, head_dim));
+}
+
+}  // namespace
+
+int hydra_attn_prefix_fwd_planned(const void* q, void* out, int64_t q_token_stride, const void* k_cache, const void* v_cache,
+                                  const int32_t* block_tables, int32_t max_blocks_per_seq, int32_t batch, int32_t n_groups, int32_t total_q,
+                                  int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t block_size, int64_t num_blocks,
+                                  float softmax_scale, void* workspace, size_t workspace_bytes, void* stream) {
+  bool done = false;
+  if (int rc = check_prefix_call(q, out, q_token_stride, k_cache, v_cache, block_tables, max_blocks_per_seq, batch, n_groups, total_q, n_q_heads, n_kv_heads,
+                                 head_dim, block_size, num_blocks, softmax_scale, workspace, workspace_bytes, &done))
+    return rc;
+  if (done) return HYDRA_OK;
+  const prefix::Layout layout = prefix::layout_of(batch, n_groups, total_q, n_q_heads / n_kv_heads, n_kv_heads, head_dim);
+  unsigned char* const ws = static_cast<unsigned char*>(workspace);
+  prefix::Args args = {};
+  args.paged.q = static_cast<const uint16_t*>(q);
+  args.paged.out = static_cast<uint16_t*>(out);
+  args.paged.q_stride = q_token_stride;
+  args.paged.k_cache = static_cast<const uint16_t*>(k_cache);
+  args.paged.v_cache = static_cast<const uint16_t*>(v_cache);
+  args.paged.block_tables = block_tables;
+  args.paged.max_blocks_per_seq = max_blocks_per_seq;
+  args.paged.num_blocks = (int32_t)num_blocks;
+  args.paged.block_shift = block_shift_of(block_size, num_blocks, max_blocks_per_seq);
+  args.paged.n_q_heads = n_q_heads;
+  args.paged.n_kv_heads = n_kv_heads;
+  args.paged.group = n_q_heads / n_kv_heads;
+  const float scale_log2 = softmax_scale * 1.44269504088896340736f;
+  args.paged.scale_log2 = scale_log2 > 1e-30f ? scale_log2 : 1e-30f;  // (a scale of 0 as a vanishing one: masked scores stay -inf)
+  args.paged.batch = batch;
+  args.header = reinterpret_cast<const prefix::PlanHeader*>(ws);
+  args.pieces = reinterpret_cast<const prefix::Piece*>(ws + layout.pieces_at);
+  args.tokens = reinterpret_cast<const prefix::Token*>(ws + layout.tokens_at);
+  args.stats = reinterpret_cast<float*>(ws + layout.stats_at);
+  args.partial_out = reinterpret_cast<float*>(ws + layout.out_at);
+  args.rows = layout.rows;
+  args.total_q = total_q;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  auto launch_for = [&](auto d) {
+    constexpr int D = decltype(d)::value;
+    hipError_t err = launch(prefix::attn_prefix_kernel<D>, dim3((unsigned)(layout.pieces * n_kv_heads)), dim3(256), s, args);
+    const int64_t merges = ((int64_t)total_q * n_q_heads + prefix::kMergeWaves - 1) / prefix::kMergeWaves;
+    if (err == hipSuccess) err = launch(prefix::prefix_merge_kernel<D>, dim3((unsigned)merges), dim3(64 * prefix::kMergeWaves), s, args);
+    return err;
+  };
+  hipError_t err;
+  switch (head_dim) {
+    case 64: err = launch_for(std::integral_constant<int, 64>{}); break;
+    case 80: err = launch_for(std::integral_constant<int, 80>{}); break;
+    default: err = launch_for(std::integral_constant<int, 128>{}); break;
+  }
+  return err == hipSuccess ? HYDRA_OK : HYDRA_ERR_LAUNCH;
+}
+
+int hydra_attn_prefix_fwd(const void* q, void* out, int64_t q_token_stride, const void* k_cache, const void* v_cache, const int32_t* block_tables,
+                          int32_t max_blocks_per_seq, const int32_t* cu_seqlens_q, const int32_t* kv_lens, const int32_t* cu_groups,
+                          const int32_t* shared_lens, int32_t batch, int32_t n_groups, int32_t total_q, int32_t n_q_heads, int32_t n_kv_heads,
+                          int32_t head_dim, int32_t block_size, int64_t num_blocks, float softmax_scale, void* workspace, size_t workspace_bytes,
+                          void* stream) {
+  // (both halves' checks before the first launch)
+  bool done = false;
+  if (int rc = check_prefix_call(q, out, q_token_stride, k_cache, v_cache, block_tables, max_blocks_per_seq, batch, n_groups, total_q, n_q_heads, n_kv_heads,
+                                 head_dim, block_size, num_blocks, softmax_scale, workspace, workspace_bytes, &done))
+    return rc;
+  if (done) return HYDRA_OK;
+  if (int rc = hydra_attn_prefix_plan(cu_seqlens_q, kv_lens, cu_groups, shared_lens, batch, n_groups, total_q, n_q_heads, n_kv_heads, head_dim, max_blocks_per_seq,
+                                      block_size, workspace, workspace_bytes, stream))
+    return rc;
+  return hydra_attn_prefix_fwd_planned(q, out, q_token_stride, k_cache, v_cache, block_tables, max_blocks_per_seq, batch, n_groups, total_q, n_q_heads, n_kv_heads,
+                                       head_dim, block_size, num_blocks, softmax_scale, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

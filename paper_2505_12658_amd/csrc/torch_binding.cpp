@@ -38,6 +38,10 @@ struct Library {
   decltype(&hydra_page_cache_gather) page_cache_gather = nullptr;
   decltype(&hydra_page_maps_build) page_maps_build = nullptr;
   decltype(&hydra_qk_norm_rope) qk_norm_rope = nullptr;
+  decltype(&hydra_attn_prefix_workspace_bytes) attn_prefix_workspace_bytes = nullptr;
+  decltype(&hydra_attn_prefix_plan) attn_prefix_plan = nullptr;
+  decltype(&hydra_attn_prefix_fwd) attn_prefix_fwd = nullptr;
+  decltype(&hydra_attn_prefix_fwd_planned) attn_prefix_fwd_planned = nullptr;
 };
 Library lib;
 PyObject* hydra_error = nullptr;  // the HydraError class: HydraError(status, where)
@@ -476,6 +480,106 @@ PyObject* py_qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// A workspace that was given, or one of `need` bytes (of the least size where the sizes are refused anyway).
+at::Tensor workspace_of(PyObject* given, size_t need, const at::Tensor& with, PyObject* stream) {
+  if (given == Py_None) {
+    const at::Tensor t = bytes_on(with, std::max<size_t>(need, 16));
+    used_on(stream, t);
+    return t;
+  }
+  const at::Tensor& t = tensor(given, "workspace");
+  if (!t.is_cuda() || !t.is_contiguous()) raise(PyExc_TypeError, "workspace must be a contiguous CUDA tensor");
+  same_device(with, {&t});
+  return t;
+}
+
+// cu_seqlens_q, kv_lens, cu_groups, shared_lens, total_q, n_q_heads, n_kv_heads, head_dim, max_blocks_per_seq, block_size, workspace, stream
+PyObject* py_attn_prefix_plan(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded("attn_prefix_plan", n, 12, [&] {
+    const at::Tensor &cu = index_array(a[0], at::kInt, "cu_seqlens_q"), &kv = index_array(a[1], at::kInt, "kv_lens"), &groups = index_array(a[2], at::kInt, "cu_groups"),
+                     &shared = index_array(a[3], at::kInt, "shared_lens");
+    same_device(cu, {&kv, &groups, &shared});
+    if (cu.numel() != kv.numel() + 1 || groups.numel() != shared.numel() + 1) raise(PyExc_ValueError, "shape mismatch between cu_seqlens_q, kv_lens, cu_groups and shared_lens");
+    const int32_t batch = size32(kv.numel()), n_groups = size32(shared.numel()), total = whole(a[4]), hq = whole(a[5]), hkv = whole(a[6]), d = whole(a[7]), width = whole(a[8]),
+                  block = whole(a[9]);
+    const c10::OptionalDeviceGuard guard(cu.device());
+    const at::Tensor ws = workspace_of(a[10], lib.attn_prefix_workspace_bytes(batch, n_groups, total, hq, hkv, d), cu, a[11]);
+    void* s = stream_on(a[11], cu.device());
+    call("hydra_attn_prefix_plan", [&] {
+      return lib.attn_prefix_plan(data<int32_t>(&cu), data<int32_t>(&kv), data<int32_t>(&groups), data<int32_t>(&shared), batch, n_groups, total, hq, hkv, d, width, block,
+                                  ws.data_ptr(), ws.nbytes(), s);
+    });
+    return THPVariable_Wrap(ws);
+  });
+}
+
+// The tensors that both attention calls over shared prefixes take.
+struct Prefixed {
+  const at::Tensor &q, &kc, &vc, &table;
+  int32_t batch, total, n_q, n_kv, d, block, width;
+  explicit Prefixed(PyObject* const* a) : q(token_major(a[0], "q")), kc(tensor(a[1], "k_cache")), vc(tensor(a[2], "v_cache")), table(index_array(a[3], at::kInt, "block_tables")) {
+    check_caches(kc, vc);
+    same_device(q, {&kc, &vc, &table});
+    if (table.dim() != 2 || kc.size(3) != q.size(2)) raise(PyExc_ValueError, "shape mismatch between q, caches and block_tables");
+    batch = size32(table.size(0));
+    total = size32(q.size(0));
+    n_q = size32(q.size(1));
+    n_kv = size32(kc.size(2));
+    d = size32(q.size(2));
+    block = size32(kc.size(1));
+    width = size32(table.size(1));
+  }
+  at::Tensor output(PyObject* given, PyObject* stream) const {
+    const at::Tensor t = out_like(given, q);
+    if (given == Py_None) used_on(stream, t);
+    else same_device(q, {&t});
+    return t;
+  }
+};
+
+// q, k_cache, v_cache, block_tables, cu_seqlens_q, kv_lens, cu_groups, shared_lens, softmax_scale, out, workspace, stream
+PyObject* py_attn_prefix_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded("attn_prefix_fwd", n, 12, [&] {
+    const Prefixed p(a);
+    const at::Tensor &cu = index_array(a[4], at::kInt, "cu_seqlens_q"), &kv = index_array(a[5], at::kInt, "kv_lens"), &groups = index_array(a[6], at::kInt, "cu_groups"),
+                     &shared = index_array(a[7], at::kInt, "shared_lens");
+    same_device(p.q, {&cu, &kv, &groups, &shared});
+    if (cu.numel() != (int64_t)p.batch + 1 || kv.numel() != p.batch || groups.numel() != shared.numel() + 1)
+      raise(PyExc_ValueError, "shape mismatch between block_tables, cu_seqlens_q, kv_lens, cu_groups and shared_lens");
+    const int32_t n_groups = size32(shared.numel());
+    const float scale = (float)real(a[8]);
+    const c10::OptionalDeviceGuard guard(p.q.device());
+    const at::Tensor out = p.output(a[9], a[11]);
+    const at::Tensor ws = workspace_of(a[10], a[10] == Py_None ? lib.attn_prefix_workspace_bytes(p.batch, n_groups, p.total, p.n_q, p.n_kv, p.d) : 0, p.q, a[11]);
+    void* s = stream_on(a[11], p.q.device());
+    call("hydra_attn_prefix_fwd", [&] {
+      return lib.attn_prefix_fwd(p.q.data_ptr(), out.data_ptr(), p.q.stride(0), p.kc.data_ptr(), p.vc.data_ptr(), data<int32_t>(&p.table), p.width, data<int32_t>(&cu),
+                                 data<int32_t>(&kv), data<int32_t>(&groups), data<int32_t>(&shared), p.batch, n_groups, p.total, p.n_q, p.n_kv, p.d, p.block, p.kc.size(0), scale,
+                                 ws.data_ptr(), ws.nbytes(), s);
+    });
+    return THPVariable_Wrap(out);
+  });
+}
+
+// q, k_cache, v_cache, block_tables, n_groups, softmax_scale, workspace, out, stream
+PyObject* py_attn_prefix_fwd_planned(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded("attn_prefix_fwd_planned", n, 9, [&] {
+    const Prefixed p(a);
+    const int32_t n_groups = whole(a[4]);
+    const float scale = (float)real(a[5]);
+    const c10::OptionalDeviceGuard guard(p.q.device());
+    if (a[6] == Py_None) raise(PyExc_TypeError, "workspace must be the one that the plan was written into");
+    const at::Tensor ws = workspace_of(a[6], 0, p.q, a[8]);
+    const at::Tensor out = p.output(a[7], a[8]);
+    void* s = stream_on(a[8], p.q.device());
+    call("hydra_attn_prefix_fwd_planned", [&] {
+      return lib.attn_prefix_fwd_planned(p.q.data_ptr(), out.data_ptr(), p.q.stride(0), p.kc.data_ptr(), p.vc.data_ptr(), data<int32_t>(&p.table), p.width, p.batch, n_groups, p.total,
+                                         p.n_q, p.n_kv, p.d, p.block, p.kc.size(0), scale, ws.data_ptr(), ws.nbytes(), s);
+    });
+    return THPVariable_Wrap(out);
+  });
+}
+
 // load(path, HydraError): opens the library and looks its entry points up
 PyObject* py_load(PyObject*, PyObject* args) {
   const char* path;
@@ -505,6 +609,10 @@ PyObject* py_load(PyObject*, PyObject* args) {
   find(l.page_cache_gather, "hydra_page_cache_gather");
   find(l.page_maps_build, "hydra_page_maps_build");
   find(l.qk_norm_rope, "hydra_qk_norm_rope");
+  find(l.attn_prefix_workspace_bytes, "hydra_attn_prefix_workspace_bytes");
+  find(l.attn_prefix_plan, "hydra_attn_prefix_plan");
+  find(l.attn_prefix_fwd, "hydra_attn_prefix_fwd");
+  find(l.attn_prefix_fwd_planned, "hydra_attn_prefix_fwd_planned");
   if (!all) {
     PyErr_Format(PyExc_ImportError, "%s lacks an entry point of hydra_attn.h or hydra_step.h", path);
     return nullptr;
@@ -528,6 +636,9 @@ PyMethodDef methods[] = {{"load", py_load, METH_VARARGS, nullptr},
                          HYDRA_FAST(page_cache_gather),
                          HYDRA_FAST(page_maps_build),
                          HYDRA_FAST(qk_norm_rope),
+                         HYDRA_FAST(attn_prefix_plan),
+                         HYDRA_FAST(attn_prefix_fwd),
+                         HYDRA_FAST(attn_prefix_fwd_planned),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_hydra_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

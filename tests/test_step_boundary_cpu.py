@@ -65,6 +65,38 @@ def test_norm_and_rotation_refusals(lib, change, status):
     assert _rope(lib, **change) == status
 
 
+def _prefix(lib, q=16, out=32, qs=128, kc=16, vc=16, table=16, width=4, cu=16, kv=16, groups=16, shared=16, batch=3, n_groups=1, total=3, hq=2, hkv=2, d=64, block=16, blocks=32,
+            scale=0.125, ws=16, ws_bytes=1 << 30):
+    return lib.hydra_attn_prefix_fwd(q, out, qs, kc, vc, table, width, cu, kv, groups, shared, batch, n_groups, total, hq, hkv, d, block, blocks, scale, ws, ws_bytes, None)
+
+
+@pytest.mark.parametrize("change, status", [
+    (dict(q=None), INVALID), (dict(out=None), INVALID), (dict(kc=None), INVALID), (dict(vc=None), INVALID), (dict(table=None), INVALID), (dict(cu=None), INVALID), (dict(kv=None), INVALID),
+    (dict(groups=None), INVALID), (dict(shared=None), INVALID), (dict(q=8), INVALID), (dict(out=8), INVALID), (dict(vc=24), INVALID), (dict(qs=120), INVALID), (dict(qs=132), INVALID),
+    (dict(batch=-1), INVALID), (dict(n_groups=-1), INVALID), (dict(n_groups=0), INVALID), (dict(total=-1), INVALID), (dict(hq=3), INVALID), (dict(hkv=0), INVALID), (dict(width=0), INVALID),
+    (dict(blocks=0), INVALID), (dict(scale=-1.0), INVALID), (dict(scale=float("nan")), INVALID), (dict(scale=float("inf")), INVALID), (dict(d=96), UNSUPPORTED),
+    (dict(batch=2049), UNSUPPORTED), (dict(n_groups=2049), UNSUPPORTED), (dict(total=(1 << 23) + 1), UNSUPPORTED), (dict(block=24), UNSUPPORTED), (dict(block=0), UNSUPPORTED),
+    (dict(blocks=1 << 27), UNSUPPORTED), (dict(width=(1 << 26) + 1), UNSUPPORTED), (dict(ws=None), WORKSPACE), (dict(ws=24), WORKSPACE), (dict(ws_bytes=1000), WORKSPACE),
+    (dict(batch=0), OK), (dict(total=0), OK), (dict(batch=0, n_groups=0), OK),
+], ids=str)
+def test_prefix_attention_refusals(lib, change, status):
+    assert _prefix(lib, **change) == status
+
+
+def test_prefix_plan_and_planned_refusals(lib):
+    plan = lambda cu=16, width=4, block=16, ws=16, n=1 << 30: lib.hydra_attn_prefix_plan(cu, 16, 16, 16, 3, 1, 3, 2, 2, 64, width, block, ws, n, None)  # noqa: E731
+    assert plan(cu=None) == INVALID and plan(width=0) == INVALID and plan(block=0) == INVALID
+    assert plan(block=12) == UNSUPPORTED and plan(ws=None) == WORKSPACE and plan(n=64) == WORKSPACE
+    run = lambda q=16, table=16, ws=16, n=1 << 30: lib.hydra_attn_prefix_fwd_planned(q, 32, 128, 16, 16, table, 4, 3, 1, 3, 2, 2, 64, 16, 32, 0.125, ws, n, None)  # noqa: E731
+    assert run(q=None) == INVALID and run(table=None) == INVALID and run(ws=None) == WORKSPACE and run(n=64) == WORKSPACE
+
+
+def test_prefix_workspace_bytes(lib):
+    size = hydra.hydra_attn_prefix_workspace_bytes
+    assert size(3, 1, 3, 3, 2, 64) == 0 and size(3, 1, 3, 2, 2, 96) == 0 and size(2049, 1, 3, 2, 2, 64) == 0
+    assert 0 < size(3, 1, 3, 2, 2, 64) < size(300, 1, 3000, 2, 2, 64) < size(300, 1, 3000, 2, 2, 128)
+
+
 def test_binding_refuses_what_is_no_gpu_tensor():
     q = torch.zeros((4, 2, 64), dtype=torch.bfloat16)
     with pytest.raises(TypeError):
