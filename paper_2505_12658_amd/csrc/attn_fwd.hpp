@@ -278,9 +278,10 @@ constexpr float kMaxRowSum = 1.0995116e12f;  // 2^40: largest row sum (relative 
 // list's queues and K/V rows from the packed batch; for small batches a workgroup works its one item out for itself
 // (attn_fwd_direct_kernel) and hands it over in its source object; the paged kernel does so as well, with K/V rows
 // gathered from cache pages and queries that are the LAST q_len positions of a context of kv_len keys (see
-// attn_paged.hpp for that source).
+// attn_paged.hpp for that source).  A source of packed rows (kPackedRows, attn_prefix.hpp) has rows that are (token, head) pairs, the heads of
+// a KV head next to each other, instead of wave tiles of one head each, and says itself where its result goes.
 struct PackedSource {
-  static constexpr bool kPaged = false, kOneItem = false;
+  static constexpr bool kPaged = false, kOneItem = false, kPackedRows = false;
   template <int D, int WAVES>
   using Loader = int;  // (of its loading waves: none)
   static constexpr int kTeams = 1, kTiles = kWavesPerItem;
@@ -294,7 +295,7 @@ struct PackedSource {
 // tiles (see attn_fwd_direct_kernel).
 template <int TEAMS, int LOADERS>
 struct DirectSource {
-  static constexpr bool kPaged = false, kOneItem = true;
+  static constexpr bool kPaged = false, kOneItem = true, kPackedRows = false;
 #if defined(__HIP_DEVICE_COMPILE__)
   template <int D, int WAVES>
   using Loader = TileLoader<D, WAVES>;
@@ -407,6 +408,28 @@ __device__ __forceinline__ bool attn_item_loop(const AttnArgs& a, const Src& src
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" : : "s"(m0), "v"(off), "s"(rsrc));
     }
   };
+  // The same for packed rows: rows q0 .. of the source's block.
+  [[maybe_unused]] auto issue_packed_q_loads = [&](int q0, int lane) {
+    if constexpr (Src::kPackedRows) {
+      const int first = src.first_row + q0, first_token = quotient(first, a.group), last_row = src.first_row + src.n_rows - 1;
+      const uint64_t base = (uint64_t)(uintptr_t)(a.q + (src.q_start + first_token) * a.q_stride + src.kv_head * a.group * D);
+      const uint32_t q_row_bytes = (uint32_t)(a.q_stride * 2);
+      u32x4_t rsrc;
+      rsrc[0] = __builtin_amdgcn_readfirstlane((uint32_t)base);
+      rsrc[1] = __builtin_amdgcn_readfirstlane((uint32_t)(base >> 32) & 0xffffu);
+      rsrc[2] = 0x7fffffffu;  // (rows past the end read the last one)
+      rsrc[3] = 0x00020000u;
+#pragma unroll
+      for (int instr = 0; instr < kRowInstr; ++instr) {
+        const int flat = instr * 64 + lane;
+        const int row = flat / G::kChunks, phys = flat % G::kChunks;
+        const int at = first + row < last_row ? first + row : last_row, token = quotient(at, a.group);
+        const uint32_t off = (uint32_t)(token - first_token) * q_row_bytes + (uint32_t)(at - token * a.group) * (D * 2) + k_swizzle<D>(row, phys) * 16;
+        const uint32_t m0 = __builtin_amdgcn_readfirstlane(q_stage + instr * 1024);
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" : : "s"(m0), "v"(off), "s"(rsrc));
+      }
+    }
+  };
   bool q_ahead = false;      // the current item's Q loads were issued at the end of the previous round
   bool own_empty = own_count <= 0;  // nothing is left to claim from this die's queue (same value in all waves)
   if constexpr (!Src::kOneItem) {
@@ -484,7 +507,7 @@ __device__ __forceinline__ bool attn_item_loop(const AttnArgs& a, const Src& src
     if (threadIdx.x == 0 && !own_empty) pending_claim = atomicAdd(&a.ctrl->queue_head[die * kHeadStride], 1);
   }
   const int n_tok_tiles = (seq_len + kWaveTileRows - 1) / kWaveTileRows;
-  const int n_wave_tiles = n_tok_tiles * a.group;
+  const int n_wave_tiles = Src::kPackedRows ? n_tok_tiles : n_tok_tiles * a.group;
 
   // this wave's tile
   int f = f0 + wave_tile;
@@ -494,21 +517,27 @@ __device__ __forceinline__ bool attn_item_loop(const AttnArgs& a, const Src& src
   // 6.83 -> 6.68, but one image 6.53 -> 6.59; head_dim 128 with four wave tiles, a request of 1000 tokens 16.0 -> 16.3.  One item per
   // workgroup only: over many items the causal kernel of head_dim 64 would spill vector registers for it)
   constexpr bool kByReciprocal = Src::kOneItem && !Src::kPaged && (TEAMS > 1 ? CAUSAL : D == 64);
-  auto token_tile = [&](int flat) { return kByReciprocal ? quotient(flat, a.group) : flat / a.group; };
+  auto token_tile = [&](int flat) { return Src::kPackedRows ? flat : kByReciprocal ? quotient(flat, a.group) : flat / a.group; };
   const int tok_tile = token_tile(f);
-  const int head = kv_head * a.group + (f - tok_tile * a.group);
+  const int head = Src::kPackedRows ? 0 : kv_head * a.group + (f - tok_tile * a.group);
   const int q0 = tok_tile * kWaveTileRows;
   const int f_last = (f0 + WT - 1 < n_wave_tiles ? f0 + WT - 1 : n_wave_tiles - 1);
   // KV tiles (of 64 keys) the workgroup streams
   const int n_kv_tiles = (kv_len + kKvTileRows - 1) / kKvTileRows;
-  const int causal_keys = shift + (token_tile(f_last) + 1) * kWaveTileRows;  // keys visible to the item's last query tile
-  const int W_all = CAUSAL && causal_keys < kv_len ? (causal_keys + kKvTileRows - 1) / kKvTileRows : n_kv_tiles;
+  // (packed rows: largest key, of the item's, that row `row` of the block sees)
+  [[maybe_unused]] auto limit_of_row = [&](int row) {
+    if constexpr (Src::kPackedRows) return src.limit + quotient(src.first_row + (row < seq_len ? row : seq_len - 1), a.group) - src.key_begin;
+    else return 0;
+  };
+  const int causal_keys = Src::kPackedRows ? limit_of_row(seq_len - 1) + 1 : shift + (token_tile(f_last) + 1) * kWaveTileRows;  // keys visible to the item's last query tile
+  const int W_all = CAUSAL && causal_keys < kv_len ? (Src::kPackedRows && causal_keys < 0 ? 0 : (causal_keys + kKvTileRows - 1) / kKvTileRows) : n_kv_tiles;
   // ... of which this team takes tiles [first_tile, first_tile + W_own); W: the most that a team takes
   const int W = (W_all + TEAMS - 1) / TEAMS, first_tile = team * W;
   const int W_own = TEAMS == 1 || first_tile + W <= W_all ? W : (first_tile < W_all ? W_all - first_tile : 0);
   const int key_base = first_tile * kKvTileRows;  // blocks, masks and limits count from here
   // key blocks this wave consumes: of the keys [0, kv_end) those of its team's tiles
-  const int kv_end = CAUSAL ? (shift + q0 + kWaveTileRows < kv_len ? shift + q0 + kWaveTileRows : kv_len) : kv_len;
+  const int last_key = Src::kPackedRows ? limit_of_row(q0 + kWaveTileRows - 1) + 1 : shift + q0 + kWaveTileRows;
+  const int kv_end = CAUSAL ? (last_key < kv_len ? (Src::kPackedRows && last_key < 0 ? 0 : last_key) : kv_len) : kv_len;
   int blocks = (kv_end - key_base + kKeyBlock - 1) / kKeyBlock;
   if constexpr (TEAMS > 1) blocks = blocks < 0 ? 0 : blocks < 2 * W_own ? blocks : 2 * W_own;
   const int NB = active ? blocks : 0;
@@ -583,7 +612,8 @@ __device__ __forceinline__ bool attn_item_loop(const AttnArgs& a, const Src& src
     k_loader.issue_next(k_ring);
   }
 
-  if (!q_ahead) issue_q_loads(seq_start, seq_len, q0, head, lane);
+  if constexpr (Src::kPackedRows) issue_packed_q_loads(q0, lane);
+  else if (!q_ahead) issue_q_loads(seq_start, seq_len, q0, head, lane);
   // Q fragments (B operand): lane (m, hf) holds query row q0 + 32*qs + m, columns hf*D/2 + 8*s .. +7, as
   // they come from memory.  The softmax scale is applied to the scores in fp32 (see softmax_half).
   const float c = a.scale_log2;
@@ -595,7 +625,7 @@ __device__ __forceinline__ bool attn_item_loop(const AttnArgs& a, const Src& src
   for (int qs = 0; qs < QS; ++qs) {
     int row = q0 + 32 * qs + m;
     row = row < seq_len ? row : seq_len - 1;
-    q_lim[qs] = (CAUSAL ? shift + row : kv_len - 1) - key_base;
+    q_lim[qs] = Src::kPackedRows ? limit_of_row(row) : (CAUSAL ? shift + row : kv_len - 1) - key_base;
 #pragma unroll
     for (int s = 0; s < KS; ++s)
       qf[qs][s] = *reinterpret_cast<const qreg_t*>(HYDRA_LDS_BYTE(q_stage + (32 * qs + m) * ROWB + k_swizzle<D>(32 * qs + m, KS * hf + s) * 16));
@@ -657,7 +687,7 @@ __device__ __forceinline__ bool attn_item_loop(const AttnArgs& a, const Src& src
 #pragma unroll
   for (int qs = 0; qs < QS; ++qs) {
     row_sum[qs] = 0.f;
-    if constexpr (TEAMS > 1) nref[qs] = -kLowest;  // (a wave tile none of whose keys are this team's)
+    if constexpr (TEAMS > 1 || Src::kPackedRows) nref[qs] = -kLowest;  // (a wave tile none of whose keys are this team's, or that sees none of the item's)
   }
 
   // LDS fragment reads; rb = key block inside the tile the address registers point at.
@@ -688,7 +718,7 @@ __device__ __forceinline__ bool attn_item_loop(const AttnArgs& a, const Src& src
         if (key > q_lim[qs]) S[qs][r] = -__builtin_inff();
     }
   };
-  const int min_lim = (CAUSAL ? shift + q0 : kv_len - 1) - key_base;
+  const int min_lim = Src::kPackedRows ? limit_of_row(q0) : (CAUSAL ? shift + q0 : kv_len - 1) - key_base;
   auto needs_mask = [&](int j) { return j * kKeyBlock + kKeyBlock - 1 > min_lim; };
 
   // Softmax of a key block whose S holds the raw scores, in 16 * QS halves of an element pair (pair = half / 2:
@@ -1036,6 +1066,13 @@ __device__ __forceinline__ bool attn_item_loop(const AttnArgs& a, const Src& src
       issue_q_loads(next_start, next_len, tile * kWaveTileRows, next_kv * a.group + (nf - tile * a.group), lane);
       q_ahead = true;
     }
+  }
+  if constexpr (Src::kPackedRows) {
+    if (active) {
+      const float sum = G::kSumsFromMatrixUnit ? row_sum[0] : sum_with_other_half(row_sum[0]);
+      src.template store<D>(a, smem, o_acc[0], -nref[0], sum, q0, wave, lane);
+    }
+    break;
   }
   // ---- epilogue: normalise, round to bf16, transpose through LDS, store whole rows ----
   // In the accumulators a lane owns one query row and scattered groups of 4 columns; stored from

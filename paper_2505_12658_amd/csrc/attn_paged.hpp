@@ -148,7 +148,7 @@ __device__ __forceinline__ void issue_tile_loads(const TileSlots<D, KEYS, STEP>&
 // LOADERS: waves that do nothing but load tiles (see attn_item_loop).
 template <int LOADERS = 0>
 struct PagedSource {
-  static constexpr bool kPaged = true, kOneItem = true;
+  static constexpr bool kPaged = true, kOneItem = true, kPackedRows = false;
   static constexpr int kTeams = 1, kTiles = kWavesPerItem;
   static constexpr int kLoaders = LOADERS, kStageRows = LOADERS > 0 ? kWavesPerItem * kWaveTileRows : 0;
   template <int D>

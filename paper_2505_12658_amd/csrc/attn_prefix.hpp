@@ -13,9 +13,10 @@ namespace prefix {
 struct Args {
   paged::PagedArgs paged;  // queries, output, cache and table as in the paged call; its lengths and shares are not used
   const PlanHeader* header;
+  const int32_t* starts;
+  const Request* requests;
   const Piece* pieces;
-  const Token* tokens;
-  float* stats;        // [n_kv_heads][rows] maximum, sum
+  float* stats;        // [n_kv_heads][rows] maximum (of exponents of two), sum
   float* partial_out;  // [n_kv_heads][rows][D]
   int64_t rows;        // of partial results of a KV head
   int32_t total_q;
@@ -23,24 +24,212 @@ struct Args {
 
 #if defined(__HIP_DEVICE_COMPILE__)
 
+__device__ __forceinline__ void store_stats(const Args& args, int64_t row, float scaled_max, float sum) {
+  *reinterpret_cast<f32x2_t*>(args.stats + 2 * row) = f32x2_t{scaled_max, sum};
+}
+__device__ __forceinline__ u32x2_t rounded(float a, float b, float c, float d) {
+  const f32x2_t lo = {a, b}, hi = {c, d};
+  return u32x2_t{__builtin_bit_cast(uint32_t, __builtin_convertvector(lo, bf16x2_t)), __builtin_bit_cast(uint32_t, __builtin_convertvector(hi, bf16x2_t))};
+}
+
+// ---- more than 64 rows: the packed kernel's pipeline (attn_fwd.hpp) --------------------------------------------------
+// A workgroup of four waves of 32 rows that share every tile of 64 keys.  The gatherer is the paged call's, from the piece's first key on.
+struct RowsSource {
+  static constexpr bool kPaged = true, kOneItem = true, kPackedRows = true;
+  static constexpr int kTeams = 1, kTiles = kWavesPerItem, kLoaders = 0, kStageRows = 0;
+  template <int D>
+  static constexpr int kWavesPerSimd = paged::kPagedWavesPerSimd;
+  const Args* args;
+  int64_t q_start;             // first token of the set
+  int first_row, n_rows;       // of the block, in the set
+  int q_len, kv_len;           // rows of the block, keys of the piece
+  int limit, key_begin, key_end, f0, kv_head, table_row, partial;
+
+  template <int D>
+  struct Gather : paged::PagedSource<0>::Gather<D> {
+    using Base = typename paged::PagedSource<0>::template Gather<D>;
+    int first_tile;
+    __device__ __forceinline__ void init(const RowsSource& src, int kv_head, int wave, int lane) {
+      paged::PagedSource<0> pages;
+      pages.args = &src.args->paged;
+      pages.table = src.args->paged.block_tables + (int64_t)src.table_row * src.args->paged.max_blocks_per_seq;
+      pages.kv_len = src.key_end;
+      Base::init(pages, kv_head, wave, lane);
+      first_tile = src.key_begin / kKvTileRows;
+      this->next_tile = first_tile;
+      this->lookup(first_tile);
+    }
+    __device__ __forceinline__ void issue_first(uint32_t k_dst) {
+      this->take(this->v_block);
+      this->issue_tile(first_tile, this->v_block, this->k_lo, this->k_hi, this->k_lane_off, k_dst);
+      this->next_tile = first_tile + 1;
+      this->lookup(first_tile + 1);
+    }
+  };
+
+  // The wave's rows q0 .. of the block: lane (m, hf) has row m's columns 32 cc + 8 g + 4 hf .. + 3 in o[cc][4 g ..].  They go
+  // through LDS (the rings, which nobody reads any more), so that whole rows are stored; 16-byte pieces are placed by an exclusive or with the
+  // row, which spreads the 32 rows' equal columns over the banks.
+  template <int D>
+  __device__ __forceinline__ void store(const AttnArgs& a, unsigned char* smem, const f32x16_t (&o)[RowGeom<D>::kPvChunks], float scaled_max, float sum, int q0, int wave,
+                                        int lane) const {
+    const int m = lane & 31, hf = lane >> 5;
+    const int rows = n_rows - q0 < kWaveTileRows ? n_rows - q0 : kWaveTileRows;
+    constexpr int kPieces = D / 4, kRowBytes = D * 4;
+    static_assert(kWavesPerItem * kWaveTileRows * kRowBytes <= 4 * RowGeom<D>::kTileBytes, "two rings of two tiles hold the rows");
+    const uint32_t stage = (uint32_t)(uintptr_t)HYDRA_LDS_PTR(smem) + wave * (kWaveTileRows * kRowBytes);
+    const bool final = partial < 0;
+    const float scale = final ? 1.0f / sum : 1.0f;
+#pragma unroll
+    for (int cc = 0; cc < RowGeom<D>::kPvChunks; ++cc)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int piece = 8 * cc + 2 * g + hf;
+        *reinterpret_cast<f32x4_t*>(HYDRA_LDS_BYTE(stage + m * kRowBytes + ((piece ^ m) % kPieces) * 16)) =
+            f32x4_t{o[cc][4 * g] * scale, o[cc][4 * g + 1] * scale, o[cc][4 * g + 2] * scale, o[cc][4 * g + 3] * scale};
+      }
+    const int64_t record = kv_head * args->rows + partial + q0;
+    if (!final && hf == 0 && m < rows) store_stats(*args, record + m, scaled_max, sum);
+    constexpr int kRowsAtOnce = 64 / kPieces;
+#pragma unroll
+    for (int i = 0; i < kWaveTileRows / kRowsAtOnce; ++i) {
+      const int r = i * kRowsAtOnce + lane / kPieces, piece = lane % kPieces;
+      const f32x4_t x = *reinterpret_cast<const f32x4_t*>(HYDRA_LDS_BYTE(stage + r * kRowBytes + ((piece ^ r) % kPieces) * 16));
+      if (r >= rows) continue;
+      if (final) {
+        const int row = first_row + q0 + r, token = quotient(row, a.group), head = kv_head * a.group + (row - token * a.group);
+        *reinterpret_cast<u32x2_t*>(a.out + ((q_start + token) * a.n_q_heads + head) * D + piece * 4) = rounded(x[0], x[1], x[2], x[3]);
+      } else {
+        *reinterpret_cast<f32x4_t*>(args->partial_out + (record + r) * D + piece * 4) = x;
+      }
+    }
+  }
+};
+
+// ---- up to 16 rows: the decode form (attn_decode.hpp) -----------------------------------------------------------------
+// The four waves take the blocks of 32 keys one after the other in turn, and their results are merged through LDS.
+template <int D>
+__device__ __forceinline__ void run_few_rows(const Args& args, const Piece& piece, int kv_head, float* lds) {
+  constexpr int kWaves = paged::kDecodeWaves, kRows = paged::kDecodeRows, kKeys = paged::kDecodeKeys;
+  const paged::PagedArgs& a = args.paged;
+  const int thread = (int)threadIdx.x, lane = thread & 63, wave = __builtin_amdgcn_readfirstlane(thread >> 6), m = lane & 15, h = lane >> 4;
+  float* const s_max = lds;
+  float* const s_sum = s_max + kWaves * kRows;
+  float* const s_slots = s_sum + kWaves * kRows;
+  const int n_rows = piece.form_rows & 255, end = piece.key_end, n_blocks = (end - piece.key_begin + kKeys - 1) / kKeys;
+  const int steps = wave < n_blocks ? (n_blocks - wave + kWaves - 1) / kWaves : 0;
+  auto key_of = [&](int i) { return piece.key_begin + (wave + kWaves * i) * kKeys; };
+  const int32_t* const table = a.block_tables + (int64_t)piece.table_row * a.max_blocks_per_seq;
+  const int last_entry = (end - 1) >> a.block_shift;
+  // (the table's entries of 32 steps at once, lane 2 i + half for that half of step i: see run_decode)
+  auto entries = [&](int first_step) {
+    const int e = (key_of(first_step + (lane >> 1)) + 16 * (lane & 1)) >> a.block_shift;
+    return table[e < last_entry ? e : last_entry];
+  };
+  int ids = entries(0);
+  const int row = piece.first_row + (m < n_rows ? m : n_rows - 1);
+  const int token = quotient(row, a.group), head = kv_head * a.group + (row - token * a.group);
+  const int limit = piece.limit + token;
+  const float c = a.scale_log2;
+  paged::DecodeWave<D> w;
+  w.init(a.k_cache, a.v_cache, a.n_kv_heads, kv_head, end, a.block_shift, a.num_blocks, a.q + (int64_t)(piece.first_token + token) * a.q_stride + head * D, c,
+         (uint32_t)(uintptr_t)HYDRA_LDS_PTR(s_slots + wave * paged::kDecodeSlotFloats<D>), lane);
+  if (steps > 0) {
+    auto in_cache = [&](int id) { return id < 0 ? 0 : (id > w.last_block ? w.last_block : id); };
+    auto id_of = [&](int i, int half) { return __builtin_amdgcn_readlane(ids, 2 * (i & 31) + half); };
+    ids = in_cache(ids);
+#pragma unroll
+    for (int half = 0; half < 2; ++half) w.load_k(half, id_of(0, half), key_of(0) + 16 * half);
+#pragma unroll
+    for (int half = 0; half < 2; ++half) w.load_v(half, id_of(0, half), key_of(0) + 16 * half);
+    for (int i = 0; i < steps; ++i) {
+      f32x4_t s[2];
+      w.stage_k();
+      // (the loads of a step that does not exist go out with nothing in range: see run_decode)
+      if ((i & 31) == 31) ids = in_cache(entries(i + 1));
+      const int b0 = id_of(i + 1, 0), b1 = id_of(i + 1, 1), next = i + 1 < steps ? key_of(i + 1) : end;
+      w.load_k(0, b0, next);
+      w.load_k(1, b1, next + 16);
+      __builtin_amdgcn_sched_barrier(0);
+      w.scores(s);
+      const bf16x8_t p = w.softmax(s, key_of(i), limit, c, h);
+      __builtin_amdgcn_sched_barrier(0);
+      w.product(p);
+      __builtin_amdgcn_sched_barrier(0);
+      w.load_v(0, b0, next);
+      w.load_v(1, b1, next + 16);
+    }
+  }
+  __builtin_amdgcn_sched_barrier(0);
+  constexpr int RF = paged::kDecodeRowFloats<D>, CW = paged::DecodeWave<D>::CW;
+  {
+    const float sum = paged::over_row_lanes(w.row_sum, [](float x, float y) { return x + y; });
+    if (h == 0) {
+      s_max[wave * kRows + m] = w.row_max;
+      s_sum[wave * kRows + m] = sum;
+    }
+    if (m < n_rows) {
+      float* mine = s_slots + wave * paged::kDecodeSlotFloats<D> + m * RF;
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int u = 0; u < CW; u += 4)  // columns (4 h + r) CW + u ..
+          *reinterpret_cast<f32x4_t*>(mine + (4 * h + r) * CW + u) = f32x4_t{w.o[u][r], w.o[u + 1][r], w.o[u + 2][r], w.o[u + 3][r]};
+    }
+  }
+  __syncthreads();
+  constexpr int kCols = D / 4;
+  for (int i = thread; i < n_rows * kCols; i += 64 * kWaves) {
+    const int r = i / kCols, col = (i - r * kCols) * 4;
+    float own_top[kWaves], own_sum[kWaves];
+    f32x4_t v[kWaves];
+#pragma unroll
+    for (int e = 0; e < kWaves; ++e) {
+      own_top[e] = s_max[e * kRows + r];
+      own_sum[e] = s_sum[e * kRows + r];
+      v[e] = *reinterpret_cast<const f32x4_t*>(s_slots + e * paged::kDecodeSlotFloats<D> + r * RF + col);
+    }
+    const float top = fmaxf(fmaxf(own_top[0], own_top[1]), fmaxf(own_top[2], own_top[3]));
+    static_assert(kWaves == 4, "four results");
+    float total = 0.f;
+    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int e = 0; e < kWaves; ++e) {
+      const float weight = fast_exp2((own_top[e] - top) * c);  // (0 for a wave that saw no key of this row)
+      total += weight * own_sum[e];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) acc[x] += weight * v[e][x];
+    }
+    if (piece.partial < 0) {
+      const int at = piece.first_row + r, of = quotient(at, a.group), hd = kv_head * a.group + (at - of * a.group);
+      const float inv = 1.0f / total;
+      *reinterpret_cast<u32x2_t*>(a.out + ((int64_t)(piece.first_token + of) * a.n_q_heads + hd) * D + col) = rounded(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+    } else {
+      const int64_t at = kv_head * args.rows + piece.partial + r;
+      if (col == 0) store_stats(args, at, reference_exponent(top, c), total);
+      *reinterpret_cast<f32x4_t*>(args.partial_out + at * D + col) = acc;
+    }
+  }
+}
+
+// ---- up to 32 rows -----------------------------------------------------------------------------------------------------
 // A block of up to 32 rows; the four waves split the keys: wave w takes the blocks of 32 keys w, w + 4, .. of the piece through a stage of its
 // own, and the four partial results are merged through LDS.
 template <int D>
-__device__ __forceinline__ void run_key_split(const Args& args, const Piece& piece, int kv_head, unsigned char* smem, float* s_stats) {
+__device__ __forceinline__ void run_key_split(const Args& args, const Piece& piece, int first_row, int n_rows, int partial, int kv_head, unsigned char* smem, float* s_stats) {
   using G = paged::StageGeom<D>;
   using W = paged::WaveTile<D, 1>;
   constexpr int kHalfKeys = kKvTileRows / 2, kWaves = paged::kWavesPerGroup;
   const paged::PagedArgs& a = args.paged;
-  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 31;
-  const int n_rows = piece.form_rows & 255;
+  const int thread = (int)threadIdx.x, lane = thread & 63, wave = __builtin_amdgcn_readfirstlane(thread >> 6), m = lane & 31;
 
   W w;
   w.init(lane, a.scale_log2);
   const bool valid = m < n_rows;
-  const int row = piece.first_row + (valid ? m : n_rows - 1);
-  const int token = row / a.group, head = kv_head * a.group + (row - token * a.group);
+  const int row = first_row + (valid ? m : n_rows - 1);
+  const int token = quotient(row, a.group), head = kv_head * a.group + (row - token * a.group);
   w.load_q(0, a.q + (int64_t)(piece.first_token + token) * a.q_stride + head * D, piece.limit + token);
-  const int first_limit = piece.limit + piece.first_row / a.group;  // of the block's first row: keys up to it need no mask
+  const int first_limit = piece.limit + quotient(first_row, a.group);  // of the block's first row: keys up to it need no mask
 
   const int32_t* table = a.block_tables + (int64_t)piece.table_row * a.max_blocks_per_seq;
   unsigned char* stage = smem + wave * G::kSlotBytes;
@@ -95,14 +284,14 @@ __device__ __forceinline__ void run_key_split(const Args& args, const Piece& pie
       w.o_acc[0][cc][i] = acc;
     }
   w.row_sum[0] = total;
-  if (piece.partial < 0) {
+  if (partial < 0) {
     w.store_row(0, valid ? a.out + ((int64_t)(piece.first_token + token) * a.n_q_heads + head) * D : nullptr);
     return;
   }
   const float sum = sum_with_other_half(total);
-  const int64_t at = kv_head * args.rows + piece.partial + m;
+  const int64_t at = kv_head * args.rows + partial + m;
   if (valid) {
-    if (w.hf == 0) *reinterpret_cast<f32x2_t*>(args.stats + 2 * at) = f32x2_t{top, sum};
+    if (w.hf == 0) store_stats(args, at, reference_exponent(top, w.c), sum);
 #pragma unroll
     for (int cc = 0; cc < W::CC; ++cc)
 #pragma unroll
@@ -117,87 +306,180 @@ __device__ __forceinline__ void run_key_split(const Args& args, const Piece& pie
 
 #endif  // __HIP_DEVICE_COMPILE__
 
-// grid: a workgroup per piece (of the plan's capacity) and KV head
+template <int D>
+constexpr int kLdsBytes = paged::StageGeom<D>::kLdsBytes > TileGeom<D>::kLdsBytes ? paged::StageGeom<D>::kLdsBytes : TileGeom<D>::kLdsBytes;
+
+// grid: a workgroup per piece (of the plan's capacity) and KV head; two to a compute unit
 template <int D>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_prefix_kernel(const Args a) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[paged::StageGeom<D>::kLdsBytes];
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[kLdsBytes<D>];
   __shared__ float s_stats[2 * 4 * 64];
-  const int number = (int)blockIdx.x / a.paged.n_kv_heads, kv_head = (int)blockIdx.x - number * a.paged.n_kv_heads;
-  if (number >= a.header->n_pieces) return;
-  const Piece piece = a.pieces[number];
-  run_key_split<D>(a, piece, kv_head, smem, s_stats);
+  const int number = __builtin_amdgcn_readfirstlane(quotient((int)blockIdx.x, a.paged.n_kv_heads)), kv_head = (int)blockIdx.x - number * a.paged.n_kv_heads;
+  // (the piece together with the number of them, and with the arguments that its first loads need)
+  const paged::const_table_t words = (paged::const_table_t)(uintptr_t)(a.pieces + number);
+  Piece piece = {words[0], words[1], words[2], words[3], words[4], words[5], words[6], words[7]};
+  int n_pieces = *(paged::const_table_t)(uintptr_t)&a.header->n_pieces;
+  asm volatile("" : "+s"(piece.table_row), "+s"(piece.key_begin), "+s"(piece.key_end), "+s"(piece.limit), "+s"(piece.first_token), "+s"(piece.first_row),
+               "+s"(piece.form_rows), "+s"(piece.partial), "+s"(n_pieces));
+  if (number >= n_pieces) return;
+  const int form = piece.form_rows >> 8, n_rows = piece.form_rows & 255;
+  if constexpr (D != 80) {
+    static_assert(paged::kDecodeWaves * paged::kDecodeLdsPerWave<D> <= (size_t)kLdsBytes<D>, "the decode form fits");
+    if (form == kFewRows) {
+      run_few_rows<D>(a, piece, kv_head, reinterpret_cast<float*>(smem));
+      return;
+    }
+    if (form == kManyRows) {
+      RowsSource src;
+      src.args = &a;
+      src.q_start = piece.first_token;
+      src.first_row = piece.first_row;
+      src.n_rows = src.q_len = n_rows;
+      src.kv_len = piece.key_end - piece.key_begin;
+      src.limit = piece.limit;
+      src.key_begin = piece.key_begin;
+      src.key_end = piece.key_end;
+      src.f0 = 0;
+      src.kv_head = kv_head;
+      src.table_row = piece.table_row;
+      src.partial = piece.partial;
+      AttnArgs fa = {};
+      fa.q = a.paged.q;
+      fa.out = a.paged.out;
+      fa.q_stride = a.paged.q_stride;
+      fa.n_q_heads = a.paged.n_q_heads;
+      fa.group = a.paged.group;
+      fa.scale_log2 = a.paged.scale_log2;
+      int* const s_claim = reinterpret_cast<int*>(s_stats);
+      if (!attn_item_loop<D, true>(fa, src, smem, s_claim, s_claim + 8)) return;
+      // (a row whose sum left the range of a fixed reference: all of them again, 32 at a time, with a running maximum)
+      __syncthreads();  // (every wave has seen the flag, which lies in the statistics' place)
+    }
+  }
+  for (int r = 0; r < n_rows; r += 32) {
+    if (r > 0) __syncthreads();
+    run_key_split<D>(a, piece, piece.first_row + r, n_rows - r < 32 ? n_rows - r : 32, piece.partial < 0 ? -1 : piece.partial + r, kv_head, smem, s_stats);
+  }
 #else
   (void)a;
 #endif
 }
 
-// Merge: a wave per (token, query head); a row's columns are dealt four to a lane, and D / 4 lanes that have them all take every
-// kStreams-th partial result.
-constexpr int kMergeWaves = 4;
+// Merge: a wave per (token, query head), one after the other where there are more than waves.  A lane has two columns, so at head_dim 64
+// the halves of the wave take every other partial result; kAtOnce results are asked for before the first is used.
+constexpr int kMergeWaves = 4, kMergeWorkgroups = 1024;
 template <int D>
 __global__ __launch_bounds__(64 * kMergeWaves) void prefix_merge_kernel(const Args a) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  constexpr int kLanes = D / 4, kStreams = 64 / kLanes, kEach = 2 * kMostParts / 64;
-  const int lane = (int)threadIdx.x & 63;
-  const int64_t unit = (int64_t)blockIdx.x * kMergeWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int t = (int)(unit / a.paged.n_q_heads), head = (int)(unit - (int64_t)t * a.paged.n_q_heads);
-  if (t >= a.total_q) return;
-  const Token token = a.tokens[t];
-  const int n = token.own.parts + token.shared.parts;
-  if (n == 0) return;  // written by its one piece, or a token without output
-  const int kv_head = head / a.paged.group, in_group = head - kv_head * a.paged.group;
-  // row of partial results of this row's part number i (the request's own ones first), and the distance to the next one's
-  auto first_of = [&](const TokenPart& p) {
-    if (p.parts == 0) return 0;
-    const int row = p.token * a.paged.group + in_group, block = row / p.rows;
-    return p.first + block * p.parts * p.rows + (row - block * p.rows);
+  constexpr int kStreams = D == 64 ? 2 : 1, kEach = 2 * kMostParts / 64, kAtOnce = 12;
+  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n_heads = a.paged.n_q_heads, group = a.paged.group, batch = a.paged.batch;
+  const int units = a.total_q * n_heads, first_unit = (int)blockIdx.x * kMergeWaves + wave;
+  // In one trip to memory: whether there is anything to merge; where the requests begin, four to a lane; and the request that a token has if all
+  // of them have one.
+  typedef __attribute__((ext_vector_type(4))) int32_t i32x4_t;
+  auto begins_of = [&](int b) { return *reinterpret_cast<const i32x4_t*>(a.starts + (b < batch ? b : 0)); };
+  auto guess_of = [&](int t) { return t < batch ? t : batch - 1; };
+  struct Words {
+    i32x4_t x, y;
   };
-  const int own = first_of(token.own), shared = first_of(token.shared);
-  const int64_t base = kv_head * a.rows;
-  auto row_of = [&](int i) { return base + (i < token.own.parts ? own + i * token.own.rows : shared + (i - token.own.parts) * token.shared.rows); };
-  // lane i: statistics of parts i and i + 64
-  f32x2_t stat[kEach];
-  float top = kLowest;
+  auto words_of = [&](int b) { return Words{reinterpret_cast<const i32x4_t*>(a.requests + b)[0], reinterpret_cast<const i32x4_t*>(a.requests + b)[1]}; };
+  int any_parts = a.header->any_parts;
+  i32x4_t begins = begins_of(4 * lane);
+  Words guessed = words_of(guess_of(quotient(first_unit, n_heads)));
+  asm volatile("" : "+v"(any_parts), "+v"(begins), "+v"(guessed.x), "+v"(guessed.y));
+  if (__builtin_amdgcn_readfirstlane(any_parts) == 0) return;
+  for (int unit = first_unit; unit < units; unit += (int)gridDim.x * kMergeWaves) {
+    const int t = quotient(unit, n_heads), head = unit - t * n_heads;
+    // the last request that begins at or before the token
+    int before = 0;
+    for (int b0 = 0; b0 < batch; b0 += 256) {
+      const int b = b0 + 4 * lane;
+      const i32x4_t here = b0 == 0 ? begins : begins_of(b);
 #pragma unroll
-  for (int e = 0; e < kEach; ++e) {
-    const int i = e * 64 + lane;
-    stat[e] = f32x2_t{kLowest, 0.f};
-    if (i < n) stat[e] = *reinterpret_cast<const f32x2_t*>(a.stats + 2 * row_of(i));
-    top = fmaxf(top, stat[e][0]);
-  }
+      for (int e = 0; e < 4; ++e) before += __builtin_popcountll(__builtin_amdgcn_ballot_w64(b + e < batch && here[e] <= t));
+    }
+    if (before == 0) continue;
+    Words w = guessed;
+    if (unit != first_unit || guess_of(t) != before - 1) w = words_of(before - 1);
+    auto same = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+    const Request r = {same(w.x[0]), same(w.x[1]), {same(w.x[2]), same(w.x[3])}, {same(w.y[0]), same(w.y[1])}, same(w.y[2]), 0};
+    const int own_parts = r.own.parts_rows >> 8, shared_parts = r.shared.parts_rows >> 8, n = own_parts + shared_parts;
+    if (t - r.first_token >= r.tokens || n == 0) continue;  // a token without output, or written by its one piece
+    const int kv_head = quotient(head, group), in_group = head - kv_head * group;
+    // row of partial results of this row's part number i (the request's own ones first), and the distance to the next one's
+    const int own_rows = r.own.parts_rows & 255, shared_rows = r.shared.parts_rows & 255;
+    auto first_of = [&](const SetParts& p, int token) {
+      const int row = token * group + in_group, rows = p.parts_rows & 255, block = rows == 1 ? 0 : row >> (31 - __builtin_clz(rows));
+      return p.first + block * (p.parts_rows >> 8) * rows + (row - block * rows);
+    };
+    const int own = first_of(r.own, t - r.first_token), shared = first_of(r.shared, t - r.first_token + r.place);
+    const int64_t base = kv_head * a.rows;
+    auto row_of = [&](int i) { return base + (i < own_parts ? own + i * own_rows : shared + (i - own_parts) * shared_rows); };
+    const int stream = kStreams == 2 ? lane >> 5 : 0, col = 2 * (kStreams == 2 ? lane & 31 : lane < D / 2 ? lane : D / 2 - 1);
+    f32x2_t v[2][kAtOnce];
+    auto load = [&](f32x2_t(&to)[kAtOnce], int i0) {
 #pragma unroll
-  for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-  float total = 0.f, weight[kEach];
+      for (int u = 0; u < kAtOnce; ++u) {
+        const int i = i0 + u * kStreams + stream;
+        to[u] = *reinterpret_cast<const f32x2_t*>(a.partial_out + row_of(i < n ? i : n - 1) * D + col);
+      }
+    };
+    load(v[0], 0);
+    // lane i: statistics of parts i and i + 64
+    f32x2_t stat[kEach];
 #pragma unroll
-  for (int e = 0; e < kEach; ++e) {
-    weight[e] = fast_exp2((stat[e][0] - top) * a.paged.scale_log2);
-    total += weight[e] * stat[e][1];
-  }
+    for (int e = 0; e < kEach; ++e) {
+      const int i = e * 64 + lane;
+      stat[e] = *reinterpret_cast<const f32x2_t*>(a.stats + 2 * row_of(i < n ? i : n - 1));
+    }
+    float top = stat[0][0];
 #pragma unroll
-  for (int d = 32; d > 0; d >>= 1) total += __shfl_xor(total, d);
-  const int stream = lane / kLanes, col = (lane - stream * kLanes) * 4;
-  f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
-  for (int i0 = 0; i0 < n; i0 += kStreams) {
-    const int i = i0 + stream;
-    const float w0 = __shfl(weight[0], i & 63), w1 = __shfl(weight[1], i & 63), w = i < 64 ? w0 : w1;
-    if (stream < kStreams && i < n) {
-      const f32x4_t v = *reinterpret_cast<const f32x4_t*>(a.partial_out + row_of(i) * D + col);
+    for (int e = 1; e < kEach; ++e) top = fmaxf(top, stat[e][0]);
 #pragma unroll
-      for (int x = 0; x < 4; ++x) acc[x] += w * v[x];
+    for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    float total = 0.f, weight[kEach];
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      weight[e] = e * 64 + lane < n ? fast_exp2(stat[e][0] - top) : 0.f;
+      total += weight[e] * stat[e][1];
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) total += __shfl_xor(total, d);
+    auto weight_of = [&](int i) {  // (0 past the last part)
+      const int w = __builtin_amdgcn_readlane(__builtin_bit_cast(int, i < 64 ? weight[0] : weight[1]), i & 63);
+      return __builtin_bit_cast(float, w);
+    };
+    f32x2_t acc = {0.f, 0.f};
+    auto add = [&](const f32x2_t(&from)[kAtOnce], int i0) {
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) {
+        const int i = i0 + u * kStreams;
+        if (i >= n) break;
+        float w = weight_of(i);
+        if constexpr (kStreams == 2) w = stream == 0 ? w : i + 1 < n ? weight_of(i + 1) : 0.f;
+        acc[0] += w * from[u][0];
+        acc[1] += w * from[u][1];
+      }
+    };
+    constexpr int kStep = kAtOnce * kStreams;
+    for (int i0 = 0; i0 < n; i0 += 2 * kStep) {
+      if (i0 + kStep < n) load(v[1], i0 + kStep);
+      add(v[0], i0);
+      if (i0 + 2 * kStep < n) load(v[0], i0 + 2 * kStep);
+      add(v[1], i0 + kStep);
+    }
+    if constexpr (kStreams == 2) {
+      acc[0] += __shfl_xor(acc[0], 32);
+      acc[1] += __shfl_xor(acc[1], 32);
+    }
+    if (kStreams == 2 ? lane < 32 : lane < D / 2) {
+      const float inv = 1.0f / total;
+      const f32x2_t x = {acc[0] * inv, acc[1] * inv};
+      *reinterpret_cast<uint32_t*>(a.paged.out + ((int64_t)t * n_heads + head) * D + col) = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2_t));
     }
   }
-  // the streams' sums, all in the first one's lanes
-  f32x4_t sum = acc;
-#pragma unroll
-  for (int s = 1; s < kStreams; ++s)
-#pragma unroll
-    for (int x = 0; x < 4; ++x) sum[x] += __shfl(acc[x], (lane + s * kLanes) & 63);
-  if (stream != 0) return;
-  const float inv = 1.0f / total;
-  const f32x2_t a0 = {sum[0] * inv, sum[1] * inv}, a1 = {sum[2] * inv, sum[3] * inv};
-  const u32x2_t pk = {__builtin_bit_cast(uint32_t, __builtin_convertvector(a0, bf16x2_t)), __builtin_bit_cast(uint32_t, __builtin_convertvector(a1, bf16x2_t))};
-  *reinterpret_cast<u32x2_t*>(a.paged.out + ((int64_t)t * a.paged.n_q_heads + head) * D + col) = pk;
 #else
   (void)a;
 #endif

@@ -208,8 +208,9 @@ int hydra_attn_prefix_plan(const int32_t* cu_seqlens_q, const int32_t* kv_lens, 
   args.cu_groups = cu_groups;
   args.shared_lens = shared_lens;
   args.header = reinterpret_cast<prefix::PlanHeader*>(ws);
+  args.starts = reinterpret_cast<int32_t*>(ws + layout.starts_at);
+  args.requests = reinterpret_cast<prefix::Request*>(ws + layout.requests_at);
   args.pieces = reinterpret_cast<prefix::Piece*>(ws + layout.pieces_at);
-  args.tokens = reinterpret_cast<prefix::Token*>(ws + layout.tokens_at);
   args.batch = batch;
   args.n_groups = n_groups;
   args.total_q = total_q;
@@ -218,6 +219,9 @@ int hydra_attn_prefix_plan(const int32_t* cu_seqlens_q, const int32_t* kv_lens, 
   args.table_keys = max_blocks_per_seq * block_size;
   args.pieces_capacity = (int32_t)layout.pieces;
   args.rows_capacity = (int32_t)layout.rows;
+  // (the decode form and the pipeline ask for rows of the cache that lie in one block: 16 keys, a load instruction's kilobyte)
+  args.few_rows = head_dim != 80 && block_size >= hydra::paged::kDecodeMinBlock;
+  args.many_rows = head_dim != 80 && block_size >= 1024 / (2 * head_dim);
   const hipError_t err = hydra::launch_lds(prefix::prefix_plan_kernel, dim3(1), dim3(prefix::kPlanThreads), prefix::plan_lds_bytes(batch, n_groups),
                                            static_cast<hipStream_t>(stream), args);
   return err == hipSuccess ? HYDRA_OK : HYDRA_ERR_LAUNCH;
@@ -241,7 +245,7 @@ int check_prefix_call(const void* q, const void* out, int64_t q_token_stride, co
   if (!q || !out || !k_cache || !v_cache || !block_tables) return HYDRA_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(out) || !aligned16(k_cache) || !aligned16(v_cache)) return HYDRA_ERR_INVALID_ARG;
   if (q_token_stride < (int64_t)n_q_heads * head_dim || (q_token_stride & 7)) return HYDRA_ERR_INVALID_ARG;
-  if (block_shift_of(block_size, num_blocks, max_blocks_per_seq) < 0) return HYDRA_ERR_UNSUPPORTED;
+  if (q_token_stride > 1 << 24 || block_shift_of(block_size, num_blocks, max_blocks_per_seq) < 0) return HYDRA_ERR_UNSUPPORTED;
   return check_prefix_workspace(workspace, workspace_bytes, prefix::layout_of(batch, n_groups, total_q, n_q_heads / n_kv_heads, n_kv_heads, head_dim));
 }
 
@@ -275,8 +279,9 @@ int hydra_attn_prefix_fwd_planned(const void* q, void* out, int64_t q_token_stri
   args.paged.scale_log2 = scale_log2 > 1e-30f ? scale_log2 : 1e-30f;  // (a scale of 0 as a vanishing one: masked scores stay -inf)
   args.paged.batch = batch;
   args.header = reinterpret_cast<const prefix::PlanHeader*>(ws);
+  args.starts = reinterpret_cast<const int32_t*>(ws + layout.starts_at);
+  args.requests = reinterpret_cast<const prefix::Request*>(ws + layout.requests_at);
   args.pieces = reinterpret_cast<const prefix::Piece*>(ws + layout.pieces_at);
-  args.tokens = reinterpret_cast<const prefix::Token*>(ws + layout.tokens_at);
   args.stats = reinterpret_cast<float*>(ws + layout.stats_at);
   args.partial_out = reinterpret_cast<float*>(ws + layout.out_at);
   args.rows = layout.rows;
@@ -285,8 +290,8 @@ int hydra_attn_prefix_fwd_planned(const void* q, void* out, int64_t q_token_stri
   auto launch_for = [&](auto d) {
     constexpr int D = decltype(d)::value;
     hipError_t err = launch(prefix::attn_prefix_kernel<D>, dim3((unsigned)(layout.pieces * n_kv_heads)), dim3(256), s, args);
-    const int64_t merges = ((int64_t)total_q * n_q_heads + prefix::kMergeWaves - 1) / prefix::kMergeWaves;
-    if (err == hipSuccess) err = launch(prefix::prefix_merge_kernel<D>, dim3((unsigned)merges), dim3(64 * prefix::kMergeWaves), s, args);
+    const int merges = (total_q * n_q_heads + prefix::kMergeWaves - 1) / prefix::kMergeWaves;
+    if (err == hipSuccess) err = launch(prefix::prefix_merge_kernel<D>, dim3((unsigned)(merges < prefix::kMergeWorkgroups ? merges : prefix::kMergeWorkgroups)), dim3(64 * prefix::kMergeWaves), s, args);
     return err;
   };
   hipError_t err;

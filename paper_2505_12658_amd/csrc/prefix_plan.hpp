@@ -11,23 +11,29 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
+#include "attn_tiles.hpp"
 #include "wave_ops.hpp"
 
 namespace hydra {
 namespace prefix {
 
 constexpr int kMostRequests = 2048;
-constexpr int kPlanThreads = 1024;
+constexpr int kPlanThreads = 512;
 constexpr int kTileKeys = 64;    // keys are cut at multiples of this behind a set's first one
 constexpr int kMostParts = 64;   // of a set's keys
 constexpr int kSlots = 512;      // workgroups that the chip holds at once, two to a compute unit
 
-// How a piece is computed.
-enum Form : int32_t { kKeySplit = 1 };
-__host__ __device__ inline constexpr int rows_of_form(int) { return 32; }
-// Cost of a tile of keys, for one block of rows.
-__host__ __device__ inline constexpr int cost_of_form(int) { return 6; }
-constexpr int kLeastCost = 12;  // of a piece: less is not worth a partial result
+// How a piece is computed (attn_prefix.hpp), and rows of a block.
+enum Form : int32_t { kFewRows = 0, kKeySplit = 1, kManyRows = 2 };
+// What takes which form: sets of up to 16 rows the first, up to kMostKeySplitRows the second.
+constexpr int kMostKeySplitRows = 32;
+// Cost of a tile of keys for a block of rows, and of a piece whatever its keys, to scale: of many rows, and of others.
+constexpr int kTileCost = 16, kPieceCost = 60, kOtherTileCost = 12, kOtherPieceCost = 24;
+constexpr int kLeastTiles = 4, kOtherLeastTiles = 2;  // of a part: less is not worth a partial result
+constexpr int kOtherMostTiles = 4;                    // of a part of few rows, where there are partial results anyway
+constexpr int kPartialTiles = 22;                     // see the plan
 
 struct Piece {
   int32_t table_row;            // request whose row of the block table the keys are found by
@@ -40,37 +46,45 @@ struct Piece {
 };
 static_assert(sizeof(Piece) == 32, "two loads");
 
-// A token's partial results: of its own request's set and of its group's.  Rows r of a set: block r / rows, whose `parts` results are
-// rows of partial results first + (block * parts + part) * rows + r % rows.
-struct TokenPart {
-  int32_t first, parts, rows, token;  // token: number in the set; parts 0: none
+// Where a request's tokens find their partial results, its own set's and its group's.  Row r of a set lies in block r / rows, whose
+// `parts` results are rows first + (block * parts + part) * rows + r % rows of partial results; parts 0: none.
+struct SetParts {
+  int32_t first;
+  int32_t parts_rows;  // parts * 256 + rows
 };
-struct Token {
-  TokenPart own, shared;
+struct Request {
+  int32_t first_token, tokens;  // tokens 0: no output
+  SetParts own, shared;
+  int32_t place;                // of its first token in the group's set
+  int32_t reserved;
 };
-static_assert(sizeof(Token) == 32, "two loads");
+static_assert(sizeof(Request) == 32, "two loads");
 
 struct PlanHeader {
-  int32_t n_pieces;
-  int32_t reserved[31];
+  int32_t n_pieces;   // for each KV head; those of many rows come first
+  int32_t any_parts;  // whether there are partial results
+  int32_t reserved[30];
 };
 
-// Workspace: header, pieces, tokens, row statistics (maximum, sum), row outputs.
+// Workspace: header, first tokens of the requests, requests, pieces, row statistics (maximum, sum), row outputs.
 struct Layout {
   int64_t pieces, rows;  // capacity: pieces for each KV head, rows of partial results of a KV head
-  size_t pieces_at, tokens_at, stats_at, out_at, total;
+  size_t starts_at, requests_at, pieces_at, stats_at, out_at, total;
 };
 inline Layout layout_of(int32_t batch, int32_t n_groups, int32_t total_q, int32_t group, int32_t n_kv_heads, int32_t head_dim) {
   Layout l;
   const int64_t sets = (int64_t)batch + n_groups, rows = 2 * (int64_t)total_q * group;  // (of a group's set and of its requests' own)
-  const int64_t cuts = kSlots / n_kv_heads + 1;  // pieces that cutting keys adds at most
+  // Pieces that cutting keys adds at most: a piece that was cut off has more than half of the cost that a workgroup slot's fair share is, or
+  // of the least that is cut off; and what padding adds to rows: up to 31 of a set, 127 of one of more than 64.
+  const int64_t cuts = 4 * kSlots / n_kv_heads + 4;
   l.pieces = sets + rows / 32 + cuts;
-  const int64_t wide = sets < rows / 64 ? sets : rows / 64;  // sets of more than 64 rows
-  l.rows = rows + 32 * sets + 128 * wide + 128 * cuts;
+  const int64_t wide = sets < rows / 64 ? sets : rows / 64, whole = rows + 32 * sets + 128 * wide;
+  l.rows = whole * kMostParts < whole + 128 * cuts ? whole * kMostParts : whole + 128 * cuts;
   auto up = [](size_t n) { return (n + 255) & ~(size_t)255; };
-  l.pieces_at = sizeof(PlanHeader);
-  l.tokens_at = l.pieces_at + up((size_t)l.pieces * sizeof(Piece));
-  l.stats_at = l.tokens_at + up((size_t)total_q * sizeof(Token));
+  l.starts_at = sizeof(PlanHeader);
+  l.requests_at = l.starts_at + up((size_t)(batch + 3) / 4 * 4 * sizeof(int32_t));
+  l.pieces_at = l.requests_at + up((size_t)batch * sizeof(Request));
+  l.stats_at = l.pieces_at + up((size_t)l.pieces * sizeof(Piece));
   l.out_at = l.stats_at + up((size_t)l.rows * n_kv_heads * 2 * sizeof(float));
   l.total = l.out_at + (size_t)l.rows * n_kv_heads * head_dim * sizeof(float);
   return l;
@@ -82,217 +96,249 @@ struct PlanArgs {
   const int32_t* cu_groups;
   const int32_t* shared_lens;
   PlanHeader* header;
+  int32_t* starts;
+  Request* requests;
   Piece* pieces;
-  Token* tokens;
   int32_t batch, n_groups, total_q, group, n_kv_heads, table_keys;
   int32_t pieces_capacity, rows_capacity;
+  int32_t few_rows, many_rows;  // whether the cache's layout allows these forms
 };
-// LDS of the plan, in words: per request offset, context, group, per group first request, keys, blocks, leader, per set end of pieces, first partial row, parts.
-inline size_t plan_lds_bytes(int32_t batch, int32_t n_groups) { return ((size_t)3 * batch + 1 + (size_t)4 * n_groups + 1 + (size_t)3 * (batch + n_groups)) * sizeof(int32_t); }
+// LDS of the plan, in words: per request offset, context, group, per group first request, shared keys, leader, per set first partial row, parts,
+// per group first piece.
+inline size_t plan_lds_bytes(int32_t batch, int32_t n_groups) { return ((size_t)3 * batch + 1 + (size_t)4 * n_groups + 1 + (size_t)2 * (batch + n_groups)) * sizeof(int32_t); }
 
 #if defined(__HIP_DEVICE_COMPILE__)
 
 struct Set {
-  int rows, keys, begin;  // rows 0: no set
-  int form, blocks, tiles;
+  int rows, keys, begin, form;  // rows 0: no set
+  int log2, blocks, tiles;  // log2: of a block's rows
+  bool many;
 };
+
+// `op` over the wave's lanes, in lane 63 (as wave_scan_add); a lane without a neighbour combines with `none`.
+template <typename Op>
+__device__ __forceinline__ int over_wave(int x, int none, Op op) {
+  auto step = [&](auto ctrl, auto rows) { x = op(x, __builtin_amdgcn_update_dpp(none, x, decltype(ctrl)::value, decltype(rows)::value, 0xf, false)); };
+  using std::integral_constant;
+  step(integral_constant<int, 0x111>{}, integral_constant<int, 0xf>{});
+  step(integral_constant<int, 0x112>{}, integral_constant<int, 0xf>{});
+  step(integral_constant<int, 0x114>{}, integral_constant<int, 0xf>{});
+  step(integral_constant<int, 0x118>{}, integral_constant<int, 0xf>{});
+  step(integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});
+  step(integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});
+  return x;
+}
 
 #endif
 
 __global__ __launch_bounds__(kPlanThreads) void prefix_plan_kernel(const PlanArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
   extern __shared__ int32_t lds[];
+  constexpr int kWaves = kPlanThreads / 64;
   const int batch = a.batch, groups = a.n_groups, sets = batch + groups;
   int32_t* const s_cu = lds;                    // [batch + 1]
   int32_t* const s_kv = s_cu + batch + 1;       // [batch], 0: the request has no output
   int32_t* const s_group = s_kv + batch;        // [batch]
   int32_t* const s_first = s_group + batch;     // [groups + 1]
   int32_t* const s_keys = s_first + groups + 1; // [groups] shared keys
-  int32_t* const s_blocks = s_keys + groups;    // [groups] blocks of 128 rows of its requests one by one
-  int32_t* const s_lead = s_blocks + groups;    // [groups] first request that has output
-  int32_t* const s_end = s_lead + groups;       // [sets] end of the set's pieces
-  int32_t* const s_partial = s_end + sets;      // [sets] first row of its partial results, -1: final results
-  int32_t* const s_parts = s_partial + sets;    // [sets]
-  __shared__ int32_t s_wave[2][kPlanThreads / 64];
-  __shared__ unsigned long long s_cost;
-  const int thread = (int)threadIdx.x, lane = thread & 63, wave = thread >> 6;
+  int32_t* const s_lead = s_keys + groups;      // [groups] first request that has output
+  int32_t* const s_at = s_lead + groups;        // [groups] first piece
+  int32_t* const s_partial = s_at + groups;     // [sets] first row of its partial results, -1: final results
+  int32_t* const s_parts = s_partial + sets;    // [sets] parts * 256 + rows of a block, 0: no pieces
+  __shared__ int32_t s_wave[3][kWaves];
+  const int thread = (int)threadIdx.x, lane = thread & 63, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
+  auto least = [](int x, int y) { return y < x ? y : x; };
 
   for (int i = thread; i <= batch; i += kPlanThreads) {
     const int at = a.cu_seqlens_q[i];
-    s_cu[i] = at < 0 ? 0 : (at > a.total_q ? a.total_q : at);
+    s_cu[i] = least(at < 0 ? 0 : at, a.total_q);
     if (i < batch) {
       const int kv = a.kv_lens[i], end = a.cu_seqlens_q[i + 1], q = end - at;
-      s_kv[i] = q > 0 && kv >= q ? (kv < a.table_keys ? kv : a.table_keys) : 0;
+      s_kv[i] = q > 0 && kv >= q ? least(kv, a.table_keys) : 0;
+      s_group[i] = 0;
     }
   }
   for (int g = thread; g <= groups; g += kPlanThreads) {
     const int at = a.cu_groups[g];
-    s_first[g] = at < 0 ? 0 : (at > batch ? batch : at);
-    if (g < groups) {
-      s_keys[g] = a.shared_lens[g];
-      s_blocks[g] = 0;
-      s_lead[g] = 0x7fffffff;
-    }
-  }
-  if (thread == 0) s_cost = 0;
-  __syncthreads();
-  // what all of a group's requests have in common, and what its tokens can all see
-  for (int b = thread; b < batch; b += kPlanThreads) {
-    int lo = 0, hi = groups - 1;  // the last group that begins at or before b
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (s_first[mid] <= b) lo = mid;
-      else hi = mid - 1;
-    }
-    s_group[b] = lo;
-    const int q = s_cu[b + 1] - s_cu[b];
-    if (s_kv[b] > 0) {
-      atomicMin(&s_keys[lo], s_kv[b] - q + 1);
-      atomicAdd(&s_blocks[lo], (q * a.group + 127) / 128);
-      atomicMin(&s_lead[lo], b);
-    }
+    s_first[g] = least(at < 0 ? 0 : at, batch);
+    if (g < groups) s_keys[g] = a.shared_lens[g];
   }
   __syncthreads();
-  for (int g = thread; g < groups; g += kPlanThreads) {
-    const int first = s_first[g], end = s_first[g + 1] < first ? first : s_first[g + 1];
-    const int rows = (s_cu[end] - s_cu[first]) * a.group;
-    // (worth it where packing the rows of several requests saves blocks of rows; a chunk of many rows fills its own)
-    const bool worth = s_lead[g] < end && 4 * s_blocks[g] >= 5 * ((rows + 127) / 128);
-    s_keys[g] = worth && s_keys[g] > 0 ? s_keys[g] / kTileKeys * kTileKeys : 0;
+  auto set_with = [&](int rows, int begin, int end) {
+    Set s;
+    s.begin = begin;
+    s.keys = end - begin;
+    s.rows = s.keys > 0 ? rows : 0;
+    const bool few = s.rows <= 16 && a.few_rows != 0;
+    s.many = s.rows > kMostKeySplitRows && a.many_rows != 0;
+    s.form = s.many ? kManyRows : few ? kFewRows : kKeySplit;
+    s.log2 = s.many ? 7 : few ? 4 : 5;
+    s.blocks = (s.rows + (1 << s.log2) - 1) >> s.log2;
+    s.tiles = s.rows > 0 ? (s.keys + kTileKeys - 1) / kTileKeys : 0;
+    return s;
+  };
+  // A wave per group: what all of its requests have in common and all of their tokens can see, and what its pieces cost uncut, those of many
+  // rows by their keys alone.
+  float many_cost = 0.f, others_cost = 0.f;
+  auto count = [&](const Set& s) {
+    if (s.many) many_cost += (float)(s.blocks * kTileCost) * (float)s.tiles;
+    else others_cost += (float)s.blocks * ((float)s.tiles * kOtherTileCost + (s.tiles > 0 ? kOtherPieceCost : 0));
+  };
+  for (int g = wave; g < groups; g += kWaves) {
+    const int first = s_first[g], end = s_first[g + 1];
+    int seen = s_keys[g], blocks = 0, lead = 0x7fffffff;
+    for (int b = first + lane; b < end; b += 64) {
+      const int kv = s_kv[b];
+      s_group[b] = g;
+      if (kv > 0) {
+        const int q = s_cu[b + 1] - s_cu[b];
+        seen = least(seen, kv - q + 1);
+        blocks += (q * a.group + 127) / 128;
+        lead = least(lead, b);
+      }
+    }
+    auto in_all = [](int x) { return __builtin_amdgcn_readlane(x, 63); };
+    seen = in_all(over_wave(seen, 0x7fffffff, least));
+    lead = in_all(over_wave(lead, 0x7fffffff, least));
+    blocks = in_all(wave_scan_add(blocks));
+    const int rows = end > first ? (s_cu[end] - s_cu[first]) * a.group : 0;
+    // Worth it where packing the rows of several requests saves enough blocks of 128, each of which takes as long with fewer rows: partial
+    // results cost 128 rows the time of kPartialTiles tiles.
+    const int tiles = seen > 0 ? seen / kTileKeys : 0, packed = (rows + 127) / 128;
+    const bool worth = rows > 0 && lead < end && (float)(blocks - packed) * (float)tiles > (float)rows * (kPartialTiles / 128.0f);
+    const int keys = worth ? tiles * kTileKeys : 0;
+    if (lane == 0) {
+      s_keys[g] = keys;
+      s_lead[g] = lead;
+      count(set_with(rows, 0, keys));
+    }
+    for (int b = first + lane; b < end; b += 64)
+      if (const int kv = s_kv[b]; kv > 0) count(set_with((s_cu[b + 1] - s_cu[b]) * a.group, keys, kv));
+  }
+  // (summed up in a fixed order, so that a batch has one plan)
+  auto sum_over_wave = [](float x) {
+    return over_wave(__builtin_bit_cast(int, x), 0, [](int u, int v) { return __builtin_bit_cast(int, __builtin_bit_cast(float, u) + __builtin_bit_cast(float, v)); });
+  };
+  const int many_sum = sum_over_wave(many_cost), others_sum = sum_over_wave(others_cost);
+  if (lane == 63) {
+    s_wave[0][wave] = many_sum;
+    s_wave[1][wave] = others_sum;
+  }
+  __syncthreads();
+  // What a piece may cost, L, so that all of them cost no more than L for each of the chip's workgroups: cut into pieces of L, of which
+  // kPieceCost each is none of the keys', the sets of many rows cost many * L / (L - kPieceCost).
+  float most;
+  {
+    float many = 0.f, others = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      many += __builtin_bit_cast(float, s_wave[0][w]);
+      others += __builtin_bit_cast(float, s_wave[1][w]);
+    }
+    const float per_slot = (float)a.n_kv_heads * (1.0f / kSlots), least_cost = (float)(kPieceCost + kLeastTiles * kTileCost);
+    float l = fmaxf((many + others) * per_slot + kPieceCost, least_cost);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) l = fmaxf((others + many * l * __builtin_amdgcn_rcpf(l - kPieceCost)) * per_slot, least_cost);
+    most = l;
   }
   __syncthreads();
 
   auto set_of = [&](int i) {
-    Set s;
-    int end;
-    if (i < groups) {
-      const int first = s_first[i], last = s_first[i + 1] < first ? first : s_first[i + 1];
-      s.begin = 0;
-      end = s_keys[i];
-      s.rows = end > 0 ? (s_cu[last] - s_cu[first]) * a.group : 0;
-    } else {
-      const int b = i - groups;
-      s.begin = s_kv[b] > 0 ? s_keys[s_group[b]] : 0;
-      end = s_kv[b];
-      s.rows = end > s.begin ? (s_cu[b + 1] - s_cu[b]) * a.group : 0;
-    }
-    s.keys = end - s.begin;
-    s.form = kKeySplit;
-    const int per = rows_of_form(s.form);
-    s.blocks = (s.rows + per - 1) / per;
-    s.tiles = s.rows > 0 ? (s.keys + kTileKeys - 1) / kTileKeys : 0;
-    return s;
+    if (i < groups) return set_with((s_cu[s_first[i + 1]] - s_cu[s_first[i]]) * a.group, 0, s_keys[i]);
+    const int b = i - groups, kv = s_kv[b];
+    return set_with((s_cu[b + 1] - s_cu[b]) * a.group, kv > 0 ? s_keys[s_group[b]] : 0, kv);
   };
-  // The cost of everything, and what a piece may cost so that the chip's workgroups have equal shares of it.  (Longer parts by as much
-  // as the last tile costs, so cutting adds at most as many pieces as there are shares.)
-  {
-    int64_t cost = 0;
-    for (int i = thread; i < sets; i += kPlanThreads) {
-      const Set s = set_of(i);
-      cost += (int64_t)s.blocks * s.tiles * cost_of_form(s.form);
-    }
-    if (cost > 0) atomicAdd(&s_cost, (unsigned long long)cost);
-  }
-  __syncthreads();
-  const int slots = kSlots / a.n_kv_heads > 0 ? kSlots / a.n_kv_heads : 1;
-  int64_t share = ((int64_t)s_cost + slots - 1) / slots;
-  if (share < kLeastCost) share = kLeastCost;
-  auto parts_of = [&](const Set& s) {
-    if (s.tiles == 0) return 0;
-    const int64_t fair = (share + cost_of_form(s.form) - 1) / cost_of_form(s.form);
-    int per = fair < s.tiles ? (int)fair : s.tiles;  // tiles of a part
-    const int least = (s.tiles + kMostParts - 1) / kMostParts;
-    if (per < least) per = least;
-    return (s.tiles + per - 1) / per;
-  };
-
-  int pieces_before = 0, rows_before = 0;
+  int many_before = 0, others_before = 0, rows_before = 0;
   for (int first = 0; first < sets; first += kPlanThreads) {
     const int i = first + thread;
-    int pieces = 0, partial_rows = 0, parts = 0;
-    bool final = false;
-    if (i < sets) {
-      const Set s = set_of(i);
-      parts = parts_of(s);
-      pieces = s.blocks * parts;
-      final = i >= groups && parts == 1 && s.begin == 0;
-      partial_rows = final ? 0 : pieces * rows_of_form(s.form);
+    const Set s = set_of(i < sets ? i : sets - 1);
+    int parts = 0;
+    if (i < sets && s.tiles > 0) {
+      // Sets of many rows are cut to the next whole number of parts, up or down: 1.4 would be two rounds of pieces where one does.  Others
+      // that leave partial results anyway are cut short, since theirs are small and a chain of tiles is what a small batch waits for.
+      const float tiles = (float)s.tiles, fewest = tiles * (1.0f / kMostParts);
+      const bool always = !s.many && (i < groups || s.begin > 0);
+      float exact = s.many ? tiles * kTileCost * __builtin_amdgcn_rcpf(most - kPieceCost) : tiles * kOtherTileCost * __builtin_amdgcn_rcpf(most - kOtherPieceCost);
+      exact = always ? fmaxf(exact, tiles * (1.0f / kOtherMostTiles)) : exact;
+      const float most_parts = tiles * (s.many ? 1.0f / kLeastTiles : 1.0f / kOtherLeastTiles);
+      parts = (int)(fmaxf(fminf(exact, most_parts), fewest) + 0.5f);
+      parts = parts < 1 ? 1 : parts > kMostParts ? kMostParts : parts;
+      const int per = quotient(s.tiles + parts - 1, parts);
+      parts = quotient(s.tiles + per - 1, per);
     }
-    int pieces_end = wave_scan_add(pieces), rows_end = wave_scan_add(partial_rows);
+    const int pieces = s.blocks * parts;
+    const bool final = i >= groups && parts == 1 && s.begin == 0;
+    const int partial_rows = final ? 0 : pieces << s.log2, many = s.many ? pieces : 0;
+    int many_end = wave_scan_add(many), others_end = wave_scan_add(pieces - many), rows_end = wave_scan_add(partial_rows);
     if (lane == 63) {
-      s_wave[0][wave] = pieces_end;
-      s_wave[1][wave] = rows_end;
+      s_wave[0][wave] = many_end;
+      s_wave[1][wave] = others_end;
+      s_wave[2][wave] = rows_end;
     }
     __syncthreads();
-    int pieces_round = 0, rows_round = 0;
+    int many_round = 0, others_round = 0, rows_round = 0;
 #pragma unroll
-    for (int w = 0; w < kPlanThreads / 64; ++w) {
-      const int pw = s_wave[0][w], rw = s_wave[1][w];
-      pieces_end += w < wave ? pw : 0;
+    for (int w = 0; w < kWaves; ++w) {
+      const int mw = s_wave[0][w], ow = s_wave[1][w], rw = s_wave[2][w];
+      many_end += w < wave ? mw : 0;
+      others_end += w < wave ? ow : 0;
       rows_end += w < wave ? rw : 0;
-      pieces_round += pw;
+      many_round += mw;
+      others_round += ow;
       rows_round += rw;
     }
+    // (a round's pieces of many rows, then its others)
+    const int partial = final ? -1 : rows_before + rows_end - partial_rows;
+    int at = many_before + others_before + (s.many ? many_end : many_round + others_end) - pieces;
     if (i < sets) {
-      s_end[i] = pieces_before + pieces_end;
-      s_partial[i] = final ? -1 : rows_before + rows_end - partial_rows;
-      s_parts[i] = parts;
+      s_partial[i] = partial;
+      s_parts[i] = parts << 8 | 1 << s.log2;
+      if (i < groups) s_at[i] = at;
     }
-    pieces_before += pieces_round;
+    if (i >= groups && parts > 0) {  // a request's own pieces
+      const int b = i - groups, token = s_cu[b], limit = s_kv[b] - (s_cu[b + 1] - token), per = quotient(s.tiles + parts - 1, parts) * kTileKeys, end = s.begin + s.keys;
+      int row = partial;
+      for (int first_row = 0; first_row < s.rows; first_row += 1 << s.log2)
+        for (int key = s.begin; key < end; key += per) {
+          if (at < a.pieces_capacity) a.pieces[at] = Piece{b, key, least(key + per, end), limit, token, first_row, s.form << 8 | least(s.rows - first_row, 1 << s.log2), row};
+          ++at;
+          row += final ? 0 : 1 << s.log2;
+        }
+    }
+    many_before += many_round;
+    others_before += others_round;
     rows_before += rows_round;
     __syncthreads();
   }
-  // (cannot be more than there is room for, unless offsets decrease)
-  const int n_pieces = pieces_before <= a.pieces_capacity && rows_before <= a.rows_capacity ? pieces_before : 0;
-  if (thread == 0) a.header->n_pieces = n_pieces;
-
-  for (int p = thread; p < n_pieces; p += kPlanThreads) {
-    int lo = 0, hi = sets - 1;  // the first set that ends behind piece p
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (s_end[mid] > p) hi = mid;
-      else lo = mid + 1;
-    }
-    const Set s = set_of(lo);
-    const int parts = s_parts[lo], number = p - (s_end[lo] - s.blocks * parts), block = number / parts, part = number - block * parts;
-    const int per = (s.tiles + parts - 1) / parts * kTileKeys, block_rows = rows_of_form(s.form);
-    const int rows = s.rows - block * block_rows < block_rows ? s.rows - block * block_rows : block_rows;
-    const bool shared = lo < groups;
-    const int request = shared ? s_lead[lo] : lo - groups;
-    Piece piece;
-    piece.table_row = request;
-    piece.key_begin = s.begin + part * per;
-    piece.key_end = part * per + per < s.keys ? piece.key_begin + per : s.begin + s.keys;
-    piece.limit = shared ? 0x3fffffff : s_kv[request] - (s_cu[request + 1] - s_cu[request]);  // (every token of a group sees all shared keys)
-    piece.first_token = shared ? s_cu[s_first[lo]] : s_cu[request];
-    piece.first_row = block * block_rows;
-    piece.form_rows = s.form * 256 + rows;
-    piece.partial = s_partial[lo] < 0 ? -1 : s_partial[lo] + number * block_rows;
-    a.pieces[p] = piece;
+  // (there is room for all of them, unless offsets decrease)
+  const int all = many_before + others_before;
+  const bool fits = all <= a.pieces_capacity && rows_before <= a.rows_capacity;
+  if (thread == 0) {
+    a.header->n_pieces = fits ? all : 0;
+    a.header->any_parts = fits && rows_before > 0;
   }
-  for (int t = thread; t < a.total_q; t += kPlanThreads) {
-    int lo = 0, hi = batch - 1;  // the first request that ends behind token t
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (s_cu[mid + 1] > t) hi = mid;
-      else lo = mid + 1;
+  // one half of the waves: the groups' pieces, a wave per group; the other: the requests
+  constexpr int kHalf = kWaves / 2;
+  if (wave < kHalf) {
+    for (int g = wave; g < groups; g += kHalf) {
+      const int parts = s_parts[g] >> 8;
+      if (parts == 0) continue;
+      const Set s = set_of(g);
+      const int at = s_at[g], pieces = s.blocks * parts, per = quotient(s.tiles + parts - 1, parts) * kTileKeys, token = s_cu[s_first[g]], lead = s_lead[g], partial = s_partial[g];
+      for (int number = lane; number < pieces; number += 64) {
+        const int block = quotient(number, parts), key = (number - block * parts) * per, first_row = block << s.log2;
+        // (every token of a group sees all shared keys)
+        if (at + number < a.pieces_capacity)
+          a.pieces[at + number] = Piece{lead, key, least(key + per, s.keys), 0x3fffffff, token, first_row, s.form << 8 | least(s.rows - first_row, 1 << s.log2), partial + (number << s.log2)};
+      }
     }
-    Token token = {};
-    if (n_pieces > 0 && s_kv[lo] > 0 && t >= s_cu[lo] && t < s_cu[lo + 1]) {
-      auto part_of = [&](int set, int first_token) {
-        TokenPart part = {};
-        if (s_parts[set] == 0 || s_partial[set] < 0) return part;
-        part.first = s_partial[set];
-        part.parts = s_parts[set];
-        part.rows = rows_of_form(set_of(set).form);
-        part.token = t - first_token;
-        return part;
-      };
-      token.own = part_of(groups + lo, s_cu[lo]);
-      const int g = s_group[lo];
-      if (s_keys[g] > 0) token.shared = part_of(g, s_cu[s_first[g]]);
-    }
-    a.tokens[t] = token;
+    return;
+  }
+  for (int b = thread - 64 * kHalf; b < batch; b += kPlanThreads - 64 * kHalf) {
+    const int set = groups + b, g = s_group[b], token = s_cu[b];
+    auto of = [&](int i) { return s_parts[i] < 256 || s_partial[i] < 0 ? SetParts{0, 1} : SetParts{s_partial[i], s_parts[i]}; };
+    a.starts[b] = token;
+    a.requests[b] = Request{token, fits && s_kv[b] > 0 ? s_cu[b + 1] - token : 0, of(set), of(g), token - s_cu[s_first[g]], 0};
   }
 #else
   (void)a;

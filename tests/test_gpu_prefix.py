@@ -225,14 +225,25 @@ def test_recorded_step_with_growing_contexts():
         assert all((got[b] == 3.0).all() for b in range(9) if lengths[b] == 0)
 
 
-def test_large_scores_and_equal_keys():
-    """Scores that lead others by far, in the prefix and behind it; rows whose keys are all the same."""
-    batch = Batch([3, 2], [256, 256], [1] * 5, [100, 40, 7, 90, 64], 7, 1, 128, seed=6)
-    rows = lambda b, j: (batch.tables[b, j // 16], j % 16)  # noqa: E731
-    for b, j in ((0, 100), (1, 280), (3, 30), (4, 300)):
-        blk, at = rows(b, j)
-        batch.k_cache[blk, at] = batch.k_cache[blk, at] * 30
+@pytest.mark.parametrize("requests, block", [(3, 16), (14, 16), (40, 16), (14, 4), (30, 2)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_large_scores_and_equal_keys(requests, block, d):
+    """Scores that lead the first keys' by far more than a fixed reference allows, in the prefix and behind it; rows whose keys are all the same."""
+    batch = Batch([requests, 2], [576, 256], [1] * (requests + 2), [100, 40, 7] + [90] * (requests - 3) + [64, 1], 7, 1, d, block, seed=6)
+    for b, j in ((0, 100), (0, 470), (1, 600), (requests, 30), (requests, 300)):
+        at = (batch.tables[b, j // block], j % block)
+        batch.k_cache[at] = batch.k_cache[at] * 60
     batch.q[2] = 0
+    batch.check(_run(batch))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_large_scores_in_chunks(d):
+    """The same for requests of many rows: whole contexts in one piece, and contexts cut in parts."""
+    batch = Batch([1, 1, 1], [0, 0, 0], [40, 70, 33], [900, 70, 1500], 7, 1, d, seed=8)
+    for b, j in ((0, 500), (1, 40), (2, 64), (2, 1400)):
+        at = (batch.tables[b, j // 16], j % 16)
+        batch.k_cache[at] = batch.k_cache[at] * 60
     batch.check(_run(batch))
 
 
