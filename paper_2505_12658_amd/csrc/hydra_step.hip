@@ -61,7 +61,7 @@ int hydra_page_maps_build(const int32_t* q_lens, const int32_t* context_lens, in
   args.block_shift = shift;
   args.num_blocks = (int32_t)num_blocks;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const unsigned grid = total_tokens > 0 ? (unsigned)((total_tokens + maps::kTokensPerWorkgroup - 1) / maps::kTokensPerWorkgroup) : 1u;
+  const unsigned grid = total_tokens > 0 ? (unsigned)((total_tokens + maps::kThreads - 1) / maps::kThreads) : 1u;
   const dim3 block(maps::kThreads);
   hipError_t err;
   if (grid > 1 && (next_context == context_lens || pool == n_free)) {
@@ -138,7 +138,7 @@ int hydra_qk_norm_rope(const void* q, const void* k, const void* v, int64_t q_to
   auto launch_for = [&](auto d, auto norm) {
     constexpr int D = decltype(d)::value;
     constexpr bool kNorm = decltype(norm)::value;
-    constexpr int kRows = rope::kRowsPerWave<D, kNorm>;
+    constexpr int kRows = rope::kRowsPerWave<D>;
     // Few tokens: as many waves as there are loads of rows, so that every wave has one trip to memory and back.
     constexpr int64_t kWavesWanted = 4096;
     const int loads = (args.n_rows + kRows - 1) / kRows;

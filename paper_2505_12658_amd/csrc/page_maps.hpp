@@ -1,9 +1,12 @@
 // Page maps of a step: blocks off the free list, block tables, slots, positions, offsets and context lengths (include/hydra_step.h).
 //
 // Two sums run over the requests, of new tokens and of new blocks; everything else follows from a request's place in them.  Every
-// workgroup takes both sums over the whole batch, 1024 requests at a time, a request per thread, and keeps the piece that
-// its own tokens lie in; a token then finds its request by a search in LDS.  So one launch does, without a second one that would wait
-// for the sums of a first: the lengths are some KB that every workgroup after the first finds in L2.
+// workgroup takes both sums over the batch, a request per thread and round, until its own tokens are past, and keeps the round that they lie in;
+// a token then finds its request in LDS.  So one launch does, without a second one that would wait for the sums of a first: the
+// lengths are some KB that every workgroup after the first finds in L2.
+//
+// What bounds it: latency, of the lengths, the barriers and the table.  us: 96 decode steps 3.1, 700 5.7, 2000 9.9; prefills of 700 tokens, 100 3.6, 400
+// 4.9, 1024 (8 MB written) 8.7.  Workgroups of 1024 threads with four tokens each instead of 256 with one: 4.6, 5.1, 9.9; 6.0, 8.0, 9.7.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -13,10 +16,8 @@
 namespace hydra {
 namespace maps {
 
-constexpr int kThreads = 1024;
-constexpr int kWaves = kThreads / 64;
-constexpr int kTokensPerWorkgroup = 2048;
-constexpr int kMostTokens = 1 << 20;  // per step: 1024 requests' sums of lengths that are held to one more than this fit 31 bits
+constexpr int kThreads = 256;  // of a workgroup: a request each per round, and a token each
+constexpr int kMostTokens = 1 << 20;  // per step: 256 requests' sums of lengths that are held to one more than this fit 31 bits, behind as many before them
 
 struct Args {
   const int32_t* q_lens;
@@ -34,20 +35,22 @@ struct Args {
   int32_t free_capacity, max_blocks_per_seq, batch, total_tokens, block_shift, num_blocks;
 };
 
-// grid: a workgroup per kTokensPerWorkgroup tokens.  TOKENS: tokens, tables and what a request gets; STATE: next_context and pool.
+// grid: a workgroup per kThreads tokens.  TOKENS: tokens, tables and what a request gets; STATE: next_context and pool.
 // Both in one launch unless several workgroups would still read what they overwrite (the same arrays as context_lens and n_free).
 template <bool TOKENS, bool STATE>
 __global__ __launch_bounds__(kThreads) void page_maps_kernel(const Args a) {
 #if defined(__HIP_DEVICE_COMPILE__)
+  constexpr int kWaves = kThreads / 64, kGroup = kThreads / 64;
   __shared__ int32_t s_end[kThreads], s_context[kThreads], s_first[kThreads];  // per request: end of its tokens, context, place of its first new block on the list
   __shared__ int32_t s_wave[2][kWaves];
   __shared__ int32_t s_taken, s_wanted;  // blocks off the list, and blocks that all the requests of the step need
-  const int thread = (int)threadIdx.x, lane = thread & 63, wave = thread >> 6;
+  const int thread = (int)threadIdx.x, lane = thread & 63, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
   const int n_free_given = *a.n_free;
   const int n_free = n_free_given < 0 ? 0 : (n_free_given > a.free_capacity ? a.free_capacity : n_free_given);
   const int in_block = (1 << a.block_shift) - 1;
-  const int begin = (int)blockIdx.x * kTokensPerWorkgroup;
-  const int end = begin + kTokensPerWorkgroup < a.total_tokens ? begin + kTokensPerWorkgroup : a.total_tokens;
+  auto least = [](int x, int y) { return y < x ? y : x; };
+  const int begin = (int)blockIdx.x * kThreads;
+  const int end = least(begin + kThreads, a.total_tokens);
   if (thread == 0) s_taken = s_wanted = 0;
   int tokens_before = 0, blocks_before = 0;  // of the requests of earlier rounds
   for (int first = 0; first < a.batch; first += kThreads) {
@@ -83,8 +86,14 @@ __global__ __launch_bounds__(kThreads) void page_maps_kernel(const Args a) {
     const int token_end = q_end < a.total_tokens ? q_end : a.total_tokens;
     if (STATE) {
       // (sums only grow, and those that are served with new blocks come before those that are not)
-      if (need > 0 && served) atomicMax(&s_taken, need_end);
-      if (need > 0 && in_step) atomicMax(&s_wanted, need_end);
+      auto last = [&](bool which, int32_t* most) {
+        const uint64_t lanes = __builtin_amdgcn_ballot_w64(which);
+        if (lanes != 0 && lane == 63 - __builtin_clzll(lanes)) atomicMax(most, need_end);
+      };
+      if (blockIdx.x == 0) {
+        last(need > 0 && served, &s_taken);
+        last(need > 0 && in_step, &s_wanted);
+      }
       if (a.next_context && blockIdx.x == 0 && b < a.batch) a.next_context[b] = served ? context + q : context;
     }
     if (TOKENS) {
@@ -102,10 +111,19 @@ __global__ __launch_bounds__(kThreads) void page_maps_kernel(const Args a) {
       const int round_begin = tokens_before > begin ? tokens_before : begin;
       int round_end = tokens_before + q_round;
       round_end = round_end < end ? round_end : end;
-      const int in_round = a.batch - first < kThreads ? a.batch - first : kThreads;
-      for (int t = round_begin + thread; t < round_end; t += kThreads) {
-        // the first request that ends behind token t
+      const int in_round = least(a.batch - first, kThreads);
+      const bool long_ones = q_round > 16 * in_round;
+      for (int t0 = round_begin + 64 * wave; t0 < round_end; t0 += kThreads) {
+        const int t = t0 + lane < round_end ? t0 + lane : round_end - 1;
+        // The token's request, the first one that ends behind it: where requests have many tokens, that of the wave's first token (of 64
+        // groups, and then of one's members), which is mostly all the others' too; otherwise by a search of each lane's own.
         int lo = 0, hi = in_round - 1;
+        if (long_ones) {
+          const int group_end = least(kGroup * lane + kGroup - 1, hi);
+          lo = kGroup * __builtin_popcountll(__builtin_amdgcn_ballot_w64(kGroup * lane <= hi && s_end[group_end] <= t0));
+          lo += __builtin_ctzll(__builtin_amdgcn_ballot_w64(s_end[least(lo + lane % kGroup, hi)] > t0));
+          if (s_end[lo] > t0 + 63) hi = lo;
+        }
         while (lo < hi) {
           const int mid = (lo + hi) >> 1;
           if (s_end[mid] > t) hi = mid;
@@ -135,6 +153,7 @@ __global__ __launch_bounds__(kThreads) void page_maps_kernel(const Args a) {
     tokens_before = tokens_before < a.total_tokens ? tokens_before : a.total_tokens;
     blocks_before += need_round;
     blocks_before = blocks_before < 1 << 29 ? blocks_before : 1 << 29;  // (more only where the tokens are beyond total_tokens)
+    if (blockIdx.x != 0 && tokens_before >= end) return;  // (the first workgroup has every request's results to write)
     __syncthreads();
   }
   if (TOKENS) {

@@ -3,9 +3,11 @@
 // One wave takes the head rows of one token, or a part of them where there are few tokens: q's, k's and v's one after the other, as
 // many at a time as its lanes hold.  A lane has two 16-byte pieces of a row that are half of the rotated part apart, so that both
 // elements of each of its eight pairs are its own, in either order of pairs (elements i and i + R/2: one from each piece;
-// 2 i and 2 i + 1: neighbours).  All rows of a token rotate by the same angles: a lane computes its eight sines and cosines once.
+// 2 i and 2 i + 1: neighbours).
 //
-// Angles: frequency / 2 pi is a fixed-point part of a turn (64 bits, whole turns dropped); times the position, modulo 2^64, that is exact
+// All rows of a token rotate by the same angles: a lane computes one pair's sine and cosine while the first rows are on their way, and
+// takes those of its eight pairs from LDS.  (Each lane its own eight: 30 000 tokens of 28 / 4 heads of 128 123 us, 65 536 of 16 heads of 80 162; so, with non-temporal stores, 98 and 125.)
+// Frequency / 2 pi is a fixed-point part of a turn (64 bits, whole turns dropped); times the position, modulo 2^64, that is exact
 // to position * 2^-62 turns, and its upper half, as a signed 32-bit part of a turn, goes to the sine, whose argument is in turns.
 //
 // What bounds it: HBM, each row is read once and written once; with a handful of tokens the two trips to memory.
@@ -20,7 +22,11 @@ namespace rope {
 
 constexpr int kMostAxes = 4;
 constexpr int kWaves = 4;      // of a workgroup
-constexpr int kRowsInFlight = 4;  // rows that a lane has loaded before it computes
+// Rows that a lane has loaded before it computes.  us with 1, 2 and 4: 28 / 4 heads of 128 with the cache write, 30 000 tokens 98, 97, 98, with
+// norms 105, 103, 120; 4 tokens 3.6, 3.9, 4.7; heads of 64, 30 000 tokens 55 whatever, with norms 64, 67, 67.  16 heads of 80, whose
+// rows leave a wave's lanes with three at a time: 65 536 tokens with 1, 2, 3, 4: 129, 127, 124, 126.
+template <int D>
+constexpr int kRowsInFlight = D == 80 ? 3 : 1;
 
 struct Args {
   const uint16_t *q, *k, *v;
@@ -40,17 +46,21 @@ struct Args {
   int32_t parts, rows_per_part;                // waves per token
 };
 
-// Lanes per row.  With a norm they are the lanes that sum_over_row knows: a power of two, three of eight idle at head_dim 80.
-template <int D, bool NORM>
-constexpr int kRowLanes = D == 80 ? (NORM ? 8 : 5) : D / 16;
-template <int D, bool NORM>
-constexpr int kRowsPerWave = 64 / kRowLanes<D, NORM>;
+template <int D>
+constexpr int kRowLanes = D / 16;  // 4, 5 or 8
+template <int D>
+constexpr int kRowsPerWave = 64 / kRowLanes<D>;
 
 #if defined(__HIP_DEVICE_COMPILE__)
 
-// Sum over the 4 or 8 neighbouring lanes of a row, in all of them.
+// Sum over the lanes of a row, in all of them; number: of the lane in its row.
 template <int LANES>
-__device__ __forceinline__ float sum_over_row(float x) {
+__device__ __forceinline__ float sum_over_row(float x, int lane, int number) {
+  if constexpr (LANES == 5) {
+    auto from = [&](float v, int ahead) { return __shfl(v, lane - number + (number + ahead < 5 ? number + ahead : number + ahead - 5)); };
+    const float two = x + from(x, 1);
+    return two + from(two, 2) + from(x, 4);
+  }
   auto add = [&](auto ctrl) { x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xf, 0xf, true)); };
   add(std::integral_constant<int, 0xB1>{});  // lanes 1 0 3 2
   add(std::integral_constant<int, 0x4E>{});  // lanes 2 3 0 1
@@ -78,19 +88,26 @@ __device__ __forceinline__ u32x4_t pack(const float (&x)[8]) {
   return piece;
 }
 
+// Both halves of a row's lines are loaded by instructions of their own.  At head_dim 128 they are whole lines, and nothing is read twice.
+template <int D>
+__device__ __forceinline__ u32x4_t load_once(const u32x4_t* from) {
+  if constexpr (D == 128) return __builtin_nontemporal_load(from);
+  else return *from;
+}
+
 #endif  // __HIP_DEVICE_COMPILE__
 
 // grid: a wave per part of a token
 template <int D, bool NORM>
 __global__ __launch_bounds__(64 * kWaves) void qk_norm_rope_kernel(const Args a) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  constexpr int LANES = kRowLanes<D, NORM>, PIECES = D / 16, ROWS = kRowsPerWave<D, NORM>;
+  constexpr int PIECES = kRowLanes<D>, ROWS = kRowsPerWave<D>;
   const int lane = (int)threadIdx.x & 63;
   const int64_t unit = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int token = (int)(unit / a.parts), part = (int)(unit - (int64_t)token * a.parts);
   if (token >= a.total_tokens) return;
-  const int lane_row = lane / LANES, piece = lane - lane_row * LANES;
-  const bool active = lane_row < ROWS && piece < PIECES;
+  const int lane_row = lane / PIECES, piece = lane - lane_row * PIECES;
+  const bool active = lane_row < ROWS;
 
   // this lane's pieces of a row: l and u hold the lower and the upper elements of rotated pairs, or elements that stay
   const int rp = a.rotary_pieces;
@@ -122,44 +139,52 @@ __global__ __launch_bounds__(64 * kWaves) void qk_norm_rope_kernel(const Args a)
   const uint16_t* v_in = a.v + (int64_t)token * a.v_stride;
   const int k_first = a.n_q_heads, v_first = a.n_q_heads + a.n_kv_heads;
 
-  float cosine[8], sine[8];
+  // this wave's cosines and sines by pair
+  __shared__ f32x4_t s_angles[kWaves][D / 4];
+  f32x2_t* const angles = reinterpret_cast<f32x2_t*>(s_angles[threadIdx.x >> 6]);
+  f32x2_t angle[8];  // of this lane's pairs
   bool have_angles = false;
-  for (int row0 = part * a.rows_per_part; row0 < row_end; row0 += ROWS * kRowsInFlight) {
-    u32x4_t low[kRowsInFlight], up[kRowsInFlight];
+  for (int row0 = part * a.rows_per_part; row0 < row_end; row0 += ROWS * kRowsInFlight<D>) {
+    u32x4_t low[kRowsInFlight<D>], up[kRowsInFlight<D>];
     auto row_of = [&](int i) { return row0 + i * ROWS + lane_row; };
 #pragma unroll
-    for (int i = 0; i < kRowsInFlight; ++i) {
+    for (int i = 0; i < kRowsInFlight<D>; ++i) {
       const int row = row_of(i);
       if (active && row < row_end) {
         const uint16_t* from = row < k_first ? q_in + (int64_t)row * D : row < v_first ? k_in + (int64_t)(row - k_first) * D : v_in + (int64_t)(row - v_first) * D;
-        low[i] = reinterpret_cast<const u32x4_t*>(from)[l];
-        up[i] = reinterpret_cast<const u32x4_t*>(from)[u];
+        low[i] = load_once<D>(reinterpret_cast<const u32x4_t*>(from) + l);
+        up[i] = load_once<D>(reinterpret_cast<const u32x4_t*>(from) + u);
       }
     }
     if (!have_angles) {
       have_angles = true;
+      if (lane < 8 * rp) {
+        int axis = a.freq_axis ? a.freq_axis[lane] : 0;
+        axis = axis < 0 ? 0 : (axis >= a.n_axes ? a.n_axes - 1 : axis);
+        const int32_t position = a.positions[(int64_t)axis * a.axis_stride + token];
+        double part_of_turn = (double)a.inv_freq[lane] * 0.15915494309189533577;  // 1 / (2 pi)
+        part_of_turn -= __builtin_rint(part_of_turn);
+        const uint64_t per_position = (uint64_t)(int64_t)(part_of_turn * 0x1p62) * 4;  // (modulo whole turns)
+        const int32_t phase = (int32_t)(((uint64_t)(int64_t)position * per_position) >> 32);
+        const float turns = (float)phase * 0x1p-32f;
+        angles[lane] = f32x2_t{__builtin_amdgcn_cosf(turns), __builtin_amdgcn_sinf(turns)};
+      }
+      // (a wave's LDS instructions are done in order: no barrier)
+      __builtin_amdgcn_wave_barrier();
       if (active && rotates) {
-        int32_t at[kMostAxes];
+        const int first = a.interleaved ? 2 * l : 4 * l, second = a.interleaved ? 2 * u : 4 * l + 2;
 #pragma unroll
-        for (int x = 0; x < kMostAxes; ++x) at[x] = a.positions[(int64_t)(x < a.n_axes ? x : 0) * a.axis_stride + token];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int pair = a.interleaved ? (i < 4 ? 4 * l + i : 4 * u + i - 4) : 8 * l + i;
-          int axis = a.freq_axis ? a.freq_axis[pair] : 0;
-          axis = axis < 0 ? 0 : (axis >= a.n_axes ? a.n_axes - 1 : axis);
-          const int32_t position = axis == 0 ? at[0] : axis == 1 ? at[1] : axis == 2 ? at[2] : at[3];
-          double part_of_turn = (double)a.inv_freq[pair] * 0.15915494309189533577;  // 1 / (2 pi)
-          part_of_turn -= __builtin_rint(part_of_turn);
-          const uint64_t per_position = (uint64_t)(int64_t)(part_of_turn * 0x1p62) * 4;  // (modulo whole turns)
-          const int32_t phase = (int32_t)(((uint64_t)(int64_t)position * per_position) >> 32);
-          const float turns = (float)phase * 0x1p-32f;
-          cosine[i] = __builtin_amdgcn_cosf(turns);
-          sine[i] = __builtin_amdgcn_sinf(turns);
+        for (int i = 0; i < 2; ++i) {
+          const f32x4_t x = s_angles[threadIdx.x >> 6][first + i], y = s_angles[threadIdx.x >> 6][second + i];
+          angle[2 * i] = f32x2_t{x[0], x[1]};
+          angle[2 * i + 1] = f32x2_t{x[2], x[3]};
+          angle[4 + 2 * i] = f32x2_t{y[0], y[1]};
+          angle[5 + 2 * i] = f32x2_t{y[2], y[3]};
         }
       }
     }
 #pragma unroll
-    for (int i = 0; i < kRowsInFlight; ++i) {
+    for (int i = 0; i < kRowsInFlight<D>; ++i) {
       const int row = row_of(i);
       const bool there = active && row < row_end, is_v = row >= v_first;
       float x[8], y[8];
@@ -172,10 +197,10 @@ __global__ __launch_bounds__(64 * kWaves) void qk_norm_rope_kernel(const Args a)
           squares = __builtin_fmaf(x[j], x[j], squares);
           squares = __builtin_fmaf(y[j], y[j], squares);
         }
-        squares = sum_over_row<LANES>(there ? squares : 0.f);
+        squares = sum_over_row<PIECES>(there ? squares : 0.f, lane, piece);
         const bool is_q = row < k_first;
         const bool normed = is_q ? a.q_weight != nullptr : a.k_weight != nullptr;
-        const float scale = normed ? 1.0f / __builtin_sqrtf(squares * (1.0f / D) + a.eps) : 1.0f;
+        const float scale = normed ? __builtin_amdgcn_rsqf(squares * (1.0f / D) + a.eps) : 1.0f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           x[j] = x[j] * scale * (is_q ? w_q[j] : w_k[j]);
@@ -193,36 +218,36 @@ __global__ __launch_bounds__(64 * kWaves) void qk_norm_rope_kernel(const Args a)
 #pragma unroll
         for (int j = 0; j < 8; j += 2) {
           const int e = j / 2;
-          xr[j] = x[j] * cosine[e] - x[j + 1] * sine[e];
-          xr[j + 1] = x[j + 1] * cosine[e] + x[j] * sine[e];
-          yr[j] = y[j] * cosine[4 + e] - y[j + 1] * sine[4 + e];
-          yr[j + 1] = y[j + 1] * cosine[4 + e] + y[j] * sine[4 + e];
+          xr[j] = x[j] * angle[e][0] - x[j + 1] * angle[e][1];
+          xr[j + 1] = x[j + 1] * angle[e][0] + x[j] * angle[e][1];
+          yr[j] = y[j] * angle[4 + e][0] - y[j + 1] * angle[4 + e][1];
+          yr[j + 1] = y[j + 1] * angle[4 + e][0] + y[j] * angle[4 + e][1];
         }
       } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          xr[j] = x[j] * cosine[j] - y[j] * sine[j];
-          yr[j] = y[j] * cosine[j] + x[j] * sine[j];
+          xr[j] = x[j] * angle[j][0] - y[j] * angle[j][1];
+          yr[j] = y[j] * angle[j][0] + x[j] * angle[j][1];
         }
       }
       if (!there) continue;
       const u32x4_t low_out = is_v ? low[i] : pack(xr), up_out = is_v ? up[i] : pack(yr);
       if (row < k_first) {
         u32x4_t* to = reinterpret_cast<u32x4_t*>(a.q_out + (int64_t)token * a.q_out_stride + (int64_t)row * D);
-        to[l] = low_out;
-        to[u] = up_out;
+        __builtin_nontemporal_store(low_out, to + l);
+        __builtin_nontemporal_store(up_out, to + u);
         continue;
       }
       const int head = is_v ? row - v_first : row - k_first;
       if (!is_v && a.k_out) {
         u32x4_t* to = reinterpret_cast<u32x4_t*>(a.k_out + (int64_t)token * a.k_out_stride + (int64_t)head * D);
-        to[l] = low_out;
-        to[u] = up_out;
+        __builtin_nontemporal_store(low_out, to + l);
+        __builtin_nontemporal_store(up_out, to + u);
       }
       if (cached) {
         u32x4_t* to = reinterpret_cast<u32x4_t*>((is_v ? a.v_cache : a.k_cache) + (slot * a.n_kv_heads + head) * D);
-        to[l] = low_out;
-        to[u] = up_out;
+        __builtin_nontemporal_store(low_out, to + l);
+        __builtin_nontemporal_store(up_out, to + u);
       }
     }
   }
