@@ -33,7 +33,7 @@ constexpr int kMostKeySplitRows = 32;
 constexpr int kTileCost = 16, kPieceCost = 60, kOtherTileCost = 12, kOtherPieceCost = 24;
 constexpr int kLeastTiles = 4, kOtherLeastTiles = 2;  // of a part: less is not worth a partial result
 constexpr int kOtherMostTiles = 4;                    // of a part of few rows, where there are partial results anyway
-constexpr int kPartialTiles = 22;                     // see the plan
+constexpr int kPartialTiles = 32;                     // see the plan
 
 struct Piece {
   int32_t table_row;            // request whose row of the block table the keys are found by

@@ -80,12 +80,23 @@ class Batch:
         assert np.isfinite(got[has]).all() and (off <= allowed).all(), f"off by {(off / allowed).max():.3f} of what is allowed"
 
 
-def _run(batch, shared=None, **kw):
+def _call(planned, q, kc, vc, table, cu, kv, groups, shared, scale, out=None, workspace=None):
+    """The whole call, which leaves small batches and long chunks to the paged kernels, or its two halves, which never do."""
     import paper_2505_12658_amd as hydra
 
-    out = hydra.hydra_attn_prefix_fwd(*batch.on_gpu(shared), **kw)
+    if not planned:
+        return hydra.hydra_attn_prefix_fwd(q, kc, vc, table, cu, kv, groups, shared, scale, out=out, workspace=workspace)
+    ws = hydra.hydra_attn_prefix_plan(cu, kv, groups, shared, q.shape[0], q.shape[1], kc.shape[2], q.shape[2], table.shape[1], kc.shape[1], workspace=workspace)
+    return hydra.hydra_attn_prefix_fwd_planned(q, kc, vc, table, shared.numel(), scale, ws, out=out)
+
+
+def _run(batch, planned, shared=None, **kw):
+    out = _call(planned, *batch.on_gpu(shared), **kw)
     torch.cuda.synchronize()
     return out
+
+
+both = pytest.mark.parametrize("planned", [True, False], ids=["planned", "whole"])
 
 
 CASES = [
@@ -110,13 +121,15 @@ CASES = [
 
 
 @pytest.mark.parametrize("case", CASES, ids=lambda c: f"{c[0][0]}of{len(c[2])}-p{max(c[1])}-q{max(c[2])}-h{c[4]}k{c[5]}-d{c[6]}-b{c[7]}")
-def test_shared_prefixes(case):
+@both
+def test_shared_prefixes(case, planned):
     batch = Batch(*case, seed=len(case[2]))
-    batch.check(_run(batch))
+    batch.check(_run(batch, planned))
 
 
-@pytest.mark.parametrize("seed", range(16))
-def test_random_groups(seed):
+@pytest.mark.parametrize("seed", range(24))
+@both
+def test_random_groups(seed, planned):
     """Random groups (empty ones, groups of one), requests without new tokens or with more new tokens than context, claims of fewer and of more shared keys
     than the tokens can see, any head grouping, head_dim and block size; workspaces full of NaN."""
     import paper_2505_12658_amd as hydra
@@ -141,35 +154,43 @@ def test_random_groups(seed):
     need = hydra.hydra_attn_prefix_workspace_bytes(n, len(sizes), sum(q_lens), hq, hkv, batch.d)
     workspace = torch.full((need // 4 + 1,), float("nan"), device=DEV).view(torch.uint8)
     out = torch.full((sum(q_lens), hq, batch.d), 5.0, dtype=torch.bfloat16, device=DEV)
-    batch.check(_run(batch, claims, out=out, workspace=workspace))
+    batch.check(_run(batch, planned, claims, out=out, workspace=workspace))
     for b, (q, k) in enumerate(zip(q_lens, batch.kv_lens)):
         if k < q:
             assert (out[batch.cu[b]: batch.cu[b + 1]] == 5.0).all()
 
 
-def test_a_claim_beyond_what_the_shortest_request_sees():
+@both
+def test_a_claim_beyond_what_the_shortest_request_sees(planned):
     """The last new token of a chunk sees all of the shared keys, its first one does not: fewer are taken as shared."""
     batch = Batch([4], [512], [1, 1, 1, 1], [70, 9, 30, 1], 7, 1, 128)
     batch.q_lens[3], batch.kv_lens[3] = 40, 500
     batch.cu = np.concatenate([[0], np.cumsum(batch.q_lens)])
     batch.q = torch.randn((43, 7, 128), generator=torch.Generator().manual_seed(1)).to(torch.bfloat16)
-    batch.check(_run(batch))
+    batch.check(_run(batch, planned))
 
 
-def test_strided_queries_and_results_bit_for_bit():
-    import paper_2505_12658_amd as hydra
-
+@both
+def test_strided_queries_and_results_bit_for_bit(planned):
     batch = Batch([6, 5], [500, 900], [1, 2, 1, 1, 3, 1, 1, 1, 1, 1, 1], [9, 80, 1, 30, 3, 500, 7, 7, 100, 1, 2], 14, 2, 128, seed=4)
     args = list(batch.on_gpu())
-    first = hydra.hydra_attn_prefix_fwd(*args)
+    first = _call(planned, *args)
     wide = torch.randn((batch.q.shape[0], 14 * 128 + 40), device=DEV).to(torch.bfloat16)
     view = wide[:, 16: 16 + 14 * 128].view(-1, 14, 128)
     view.copy_(args[0])
     args[0] = view
     for _ in range(3):
-        again = hydra.hydra_attn_prefix_fwd(*args)
+        again = _call(planned, *args)
         assert torch.equal(first.view(torch.int16), again.view(torch.int16))
     batch.check(first)
+
+
+def test_large_batches_are_planned_by_the_whole_call():
+    """Contexts beyond what is sooner read one by one: the whole call gives the halves' bits."""
+    batch = Batch([12], [2048], [1] * 12, [9 + 5 * i for i in range(12)], 32, 32, 128, seed=5)
+    whole, planned = _run(batch, False), _run(batch, True)
+    batch.check(whole)
+    assert torch.equal(whole.view(torch.int16), planned.view(torch.int16))
 
 
 def test_one_plan_for_several_layers():
@@ -184,11 +205,10 @@ def test_one_plan_for_several_layers():
         q, kc, vc, table, *_ = layer.on_gpu()
         planned = hydra.hydra_attn_prefix_fwd_planned(q, kc, vc, table, 2, scale, ws)
         layer.check(planned)
-        whole = hydra.hydra_attn_prefix_fwd(q, kc, vc, table, cu, kv, groups, shared, scale)
-        assert torch.equal(planned.view(torch.int16), whole.view(torch.int16))
 
 
-def test_recorded_step_with_growing_contexts():
+@both
+def test_recorded_step_with_growing_contexts(planned):
     """Planned and run inside a graph: replays act on the lengths, groups and queries that the buffers hold by then."""
     import paper_2505_12658_amd as hydra
 
@@ -198,7 +218,7 @@ def test_recorded_step_with_growing_contexts():
     ws = torch.empty(hydra.hydra_attn_prefix_workspace_bytes(9, 2, 9, 28, 4, 128), dtype=torch.uint8, device=DEV)
 
     def step():
-        hydra.hydra_attn_prefix_fwd(q, kc, vc, table, cu, kv, groups, shared, scale, out=out, workspace=ws)
+        _call(planned, q, kc, vc, table, cu, kv, groups, shared, scale, out=out, workspace=ws)
 
     step()
     torch.cuda.synchronize()
@@ -227,24 +247,26 @@ def test_recorded_step_with_growing_contexts():
 
 @pytest.mark.parametrize("requests, block", [(3, 16), (14, 16), (40, 16), (14, 4), (30, 2)])
 @pytest.mark.parametrize("d", [64, 128])
-def test_large_scores_and_equal_keys(requests, block, d):
+@both
+def test_large_scores_and_equal_keys(requests, block, d, planned):
     """Scores that lead the first keys' by far more than a fixed reference allows, in the prefix and behind it; rows whose keys are all the same."""
     batch = Batch([requests, 2], [576, 256], [1] * (requests + 2), [100, 40, 7] + [90] * (requests - 3) + [64, 1], 7, 1, d, block, seed=6)
     for b, j in ((0, 100), (0, 470), (1, 600), (requests, 30), (requests, 300)):
         at = (batch.tables[b, j // block], j % block)
         batch.k_cache[at] = batch.k_cache[at] * 60
     batch.q[2] = 0
-    batch.check(_run(batch))
+    batch.check(_run(batch, planned))
 
 
 @pytest.mark.parametrize("d", [64, 128])
-def test_large_scores_in_chunks(d):
+@both
+def test_large_scores_in_chunks(d, planned):
     """The same for requests of many rows: whole contexts in one piece, and contexts cut in parts."""
     batch = Batch([1, 1, 1], [0, 0, 0], [40, 70, 33], [900, 70, 1500], 7, 1, d, seed=8)
     for b, j in ((0, 500), (1, 40), (2, 64), (2, 1400)):
         at = (batch.tables[b, j // 16], j % 16)
         batch.k_cache[at] = batch.k_cache[at] * 60
-    batch.check(_run(batch))
+    batch.check(_run(batch, planned))
 
 
 def test_binding_refuses_mismatched_tensors():
