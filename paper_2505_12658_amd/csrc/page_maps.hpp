@@ -53,12 +53,18 @@ __global__ __launch_bounds__(kThreads) void page_maps_kernel(const Args a) {
   const int end = least(begin + kThreads, a.total_tokens);
   if (thread == 0) s_taken = s_wanted = 0;
   int tokens_before = 0, blocks_before = 0;  // of the requests of earlier rounds
+  int q_next = 0, context_next = 0;  // the next round's lengths, on their way during this one
+  if (thread < a.batch) {
+    q_next = a.q_lens[thread];
+    context_next = a.context_lens[thread];
+  }
   for (int first = 0; first < a.batch; first += kThreads) {
     const int b = first + thread;
-    int q = 0, context = 0;
-    if (b < a.batch) {
-      q = a.q_lens[b];
-      context = a.context_lens[b];
+    int q = b < a.batch ? q_next : 0;
+    const int context = b < a.batch ? context_next : 0;
+    if (b + kThreads < a.batch) {
+      q_next = a.q_lens[b + kThreads];
+      context_next = a.context_lens[b + kThreads];
     }
     q = q < 0 ? 0 : (q > kMostTokens ? kMostTokens + 1 : q);
     const bool fits_row = context >= 0 && (int64_t)context + q <= (int64_t)a.max_blocks_per_seq << a.block_shift;
