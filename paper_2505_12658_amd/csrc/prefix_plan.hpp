@@ -33,6 +33,7 @@ constexpr int kMostKeySplitRows = 32;
 constexpr int kTileCost = 16, kPieceCost = 60, kOtherTileCost = 12, kOtherPieceCost = 24;
 constexpr int kLeastTiles = 4, kOtherLeastTiles = 2;  // of a part: less is not worth a partial result
 constexpr int kOtherMostTiles = 4;                    // of a part of few rows, where there are partial results anyway
+constexpr int kOtherRounds = 2;                       // and how many such parts the chip's workgroups take one after the other
 constexpr int kPartialTiles = 32;                     // see the plan
 
 struct Piece {
@@ -74,11 +75,13 @@ struct Layout {
 inline Layout layout_of(int32_t batch, int32_t n_groups, int32_t total_q, int32_t group, int32_t n_kv_heads, int32_t head_dim) {
   Layout l;
   const int64_t sets = (int64_t)batch + n_groups, rows = 2 * (int64_t)total_q * group;  // (of a group's set and of its requests' own)
-  // Pieces that cutting keys adds at most: a piece that was cut off has more than half of the cost that a workgroup slot's fair share is, or
-  // of the least that is cut off; and what padding adds to rows: up to 31 of a set, 127 of one of more than 64.
+  // Pieces that cutting keys adds at most, for each of the kSlots workgroups: what a piece may cost (see the plan) gives one of many rows or
+  // L / (L - kOtherPieceCost) <= 1.25 others, and parts that are cut short anyway add kOtherRounds.  What padding adds to rows: up to 31 of a set,
+  // 127 of one of more than 32.
+  static_assert(kOtherPieceCost * 5 <= kPieceCost + kLeastTiles * kTileCost && kOtherRounds <= 2, "four are enough");
   const int64_t cuts = 4 * kSlots / n_kv_heads + 4;
   l.pieces = sets + rows / 32 + cuts;
-  const int64_t wide = sets < rows / 64 ? sets : rows / 64, whole = rows + 32 * sets + 128 * wide;
+  const int64_t wide = sets < rows / 32 ? sets : rows / 32, whole = rows + 32 * sets + 128 * wide;
   l.rows = whole * kMostParts < whole + 128 * cuts ? whole * kMostParts : whole + 128 * cuts;
   auto up = [](size_t n) { return (n + 255) & ~(size_t)255; };
   l.starts_at = sizeof(PlanHeader);
@@ -227,7 +230,7 @@ __global__ __launch_bounds__(kPlanThreads) void prefix_plan_kernel(const PlanArg
   __syncthreads();
   // What a piece may cost, L, so that all of them cost no more than L for each of the chip's workgroups: cut into pieces of L, of which
   // kPieceCost each is none of the keys', the sets of many rows cost many * L / (L - kPieceCost).
-  float most;
+  float most, most_tiles;
   {
     float many = 0.f, others = 0.f;
 #pragma unroll
@@ -240,6 +243,8 @@ __global__ __launch_bounds__(kPlanThreads) void prefix_plan_kernel(const PlanArg
 #pragma unroll
     for (int i = 0; i < 4; ++i) l = fmaxf((others + many * l * __builtin_amdgcn_rcpf(l - kPieceCost)) * per_slot, least_cost);
     most = l;
+    // (at most kOtherRounds pieces of others for each workgroup that the chip holds)
+    most_tiles = fmaxf((float)kOtherMostTiles, others * per_slot * (1.0f / (kOtherTileCost * kOtherRounds)));
   }
   __syncthreads();
 
@@ -256,12 +261,12 @@ __global__ __launch_bounds__(kPlanThreads) void prefix_plan_kernel(const PlanArg
     if (i < sets && s.tiles > 0) {
       // Sets of many rows are cut to the next whole number of parts, up or down: 1.4 would be two rounds of pieces where one does.  Others
       // that leave partial results anyway are cut short, since theirs are small and a chain of tiles is what a small batch waits for.
-      const float tiles = (float)s.tiles, fewest = tiles * (1.0f / kMostParts);
+      const float tiles = (float)s.tiles;
       const bool always = !s.many && (i < groups || s.begin > 0);
       float exact = s.many ? tiles * kTileCost * __builtin_amdgcn_rcpf(most - kPieceCost) : tiles * kOtherTileCost * __builtin_amdgcn_rcpf(most - kOtherPieceCost);
-      exact = always ? fmaxf(exact, tiles * (1.0f / kOtherMostTiles)) : exact;
+      exact = always ? fmaxf(exact, tiles * __builtin_amdgcn_rcpf(most_tiles)) : exact;
       const float most_parts = tiles * (s.many ? 1.0f / kLeastTiles : 1.0f / kOtherLeastTiles);
-      parts = (int)(fmaxf(fminf(exact, most_parts), fewest) + 0.5f);
+      parts = (int)(fminf(exact, most_parts) + 0.5f);
       parts = parts < 1 ? 1 : parts > kMostParts ? kMostParts : parts;
       const int per = quotient(s.tiles + parts - 1, parts);
       parts = quotient(s.tiles + per - 1, per);

@@ -269,6 +269,31 @@ def test_large_scores_in_chunks(d, planned):
     batch.check(_run(batch, planned))
 
 
+@pytest.mark.parametrize("prefix, own, requests, q_len", [(2048, 3000, 300, 1), (0, 40000, 300, 1), (512, 9000, 500, 2), (1024, 3000, 60, 33)],
+                         ids=["behind-a-prefix", "long", "pairs", "chunks"])
+@both
+def test_workspaces_hold_the_plans_of_many_long_contexts(prefix, own, requests, q_len, planned):
+    """Many requests with long contexts of their own, which could be cut into more pieces than the chip has places for.  Eight requests over and over, so
+    that eight tell what all of them give."""
+    kinds, d, block = 8, 64, 16
+    few = Batch([kinds], [prefix], [q_len] * kinds, [own - 150 * i for i in range(kinds)], 1, 1, d, block, seed=3)
+    many = np.arange(requests) % kinds
+    rows = (many[:, None] * q_len + np.arange(q_len)).ravel()
+    args = list(few.on_gpu())
+    args[0] = args[0][torch.from_numpy(rows).to(DEV)].contiguous()
+    args[3], args[5] = args[3][torch.from_numpy(many).to(DEV)].contiguous(), _i32(np.asarray(few.kv_lens)[many])
+    args[4], args[6] = _i32(np.arange(requests + 1) * q_len), _i32([0, requests])
+    out = torch.full_like(args[0], float("nan"))
+    _call(planned, *args, out=out)
+    torch.cuda.synchronize()
+    n = kinds * q_len
+    results = few.want(), few.want(np.abs(_f64(few.v_cache)))
+    few.want = lambda values=None, q=None: results[values is not None]
+    for first in range(0, len(out), n):  # (rows of the last, broken-off turn are compared with the first turn's)
+        here = out[first: first + n]
+        few.check(torch.cat([here, out[len(here): n]]))
+
+
 def test_binding_refuses_mismatched_tensors():
     import paper_2505_12658_amd as hydra
 
