@@ -29,11 +29,12 @@ constexpr int kSlots = 512;      // workgroups that the chip holds at once, two 
 enum Form : int32_t { kFewRows = 0, kKeySplit = 1, kManyRows = 2 };
 // What takes which form: sets of up to 16 rows the first, up to kMostKeySplitRows the second.
 constexpr int kMostKeySplitRows = 32;
-// Cost of a tile of keys for a block of rows, and of a piece whatever its keys, to scale: of many rows, and of others.
-constexpr int kTileCost = 16, kPieceCost = 60, kOtherTileCost = 12, kOtherPieceCost = 24;
+// Cost of a tile of keys for a block of rows, and of a piece whatever its keys, to scale: of many rows, and of others.  A tile of a full chip takes
+// 1.2 us for each workgroup.  kPieceCost 30, 45, 60, 80: 128 requests behind 16384 keys (28 / 4 heads of 128) 53.3, 53.6, 54.3, 57.2 us, 64 of them 33.1, 34.8, 35.3, 35.1,
+// 128 behind 8192 37.0, 36.5, 37.3, 39.5; kOtherTileCost 12, 8, 6: 96 in 12 groups behind 600 .. 1800 keys 18.3, 22.0, 22.8.
+constexpr int kTileCost = 16, kPieceCost = 30, kOtherTileCost = 12, kOtherPieceCost = 24;
 constexpr int kLeastTiles = 4, kOtherLeastTiles = 2;  // of a part: less is not worth a partial result
 constexpr int kOtherMostTiles = 4;                    // of a part of few rows, where there are partial results anyway
-constexpr int kOtherRounds = 2;                       // and how many such parts the chip's workgroups take one after the other
 constexpr int kPartialTiles = 32;                     // see the plan
 
 struct Piece {
@@ -75,11 +76,11 @@ struct Layout {
 inline Layout layout_of(int32_t batch, int32_t n_groups, int32_t total_q, int32_t group, int32_t n_kv_heads, int32_t head_dim) {
   Layout l;
   const int64_t sets = (int64_t)batch + n_groups, rows = 2 * (int64_t)total_q * group;  // (of a group's set and of its requests' own)
-  // Pieces that cutting keys adds at most, for each of the kSlots workgroups: what a piece may cost (see the plan) gives one of many rows or
-  // L / (L - kOtherPieceCost) <= 1.25 others, and parts that are cut short anyway add kOtherRounds.  What padding adds to rows: up to 31 of a set,
-  // 127 of one of more than 32.
-  static_assert(kOtherPieceCost * 5 <= kPieceCost + kLeastTiles * kTileCost && kOtherRounds <= 2, "four are enough");
-  const int64_t cuts = 4 * kSlots / n_kv_heads + 4;
+  // Pieces that cutting keys adds at most, for each of the kSlots workgroups: what a piece may cost, L, gives one of many rows or
+  // L / (L - kOtherPieceCost) <= 1.5 others, and parts that are cut short anyway add one.  What padding adds to rows: up to 31 of a set, 127 of one of
+  // more than 32.
+  static_assert(kOtherPieceCost * 3 <= kPieceCost + kLeastTiles * kTileCost, "1.5");
+  const int64_t cuts = 5 * kSlots / (2 * n_kv_heads) + 4;
   l.pieces = sets + rows / 32 + cuts;
   const int64_t wide = sets < rows / 32 ? sets : rows / 32, whole = rows + 32 * sets + 128 * wide;
   l.rows = whole * kMostParts < whole + 128 * cuts ? whole * kMostParts : whole + 128 * cuts;
@@ -243,8 +244,8 @@ __global__ __launch_bounds__(kPlanThreads) void prefix_plan_kernel(const PlanArg
 #pragma unroll
     for (int i = 0; i < 4; ++i) l = fmaxf((others + many * l * __builtin_amdgcn_rcpf(l - kPieceCost)) * per_slot, least_cost);
     most = l;
-    // (at most kOtherRounds pieces of others for each workgroup that the chip holds)
-    most_tiles = fmaxf((float)kOtherMostTiles, others * per_slot * (1.0f / (kOtherTileCost * kOtherRounds)));
+    // (and parts that are cut short no shorter than gives each workgroup one of them)
+    most_tiles = fmaxf((float)kOtherMostTiles, others * per_slot * (1.0f / kOtherTileCost));
   }
   __syncthreads();
 
