@@ -184,9 +184,9 @@ __global__ __launch_bounds__(kPlanThreads) void prefix_plan_kernel(const PlanArg
   // A wave per group: what all of its requests have in common and all of their tokens can see, and what its pieces cost uncut, those of many
   // rows by their keys alone.
   float many_cost = 0.f, others_cost = 0.f;
-  auto count = [&](const Set& s) {
-    if (s.many) many_cost += (float)(s.blocks * kTileCost) * (float)s.tiles;
-    else others_cost += (float)s.blocks * ((float)s.tiles * kOtherTileCost + (s.tiles > 0 ? kOtherPieceCost : 0));
+  auto cost_of = [](const Set& s) {
+    const float tiles = (float)s.tiles;
+    return (float)s.blocks * (s.many ? tiles * kTileCost : tiles * kOtherTileCost + (s.tiles > 0 ? kOtherPieceCost : 0.f));
   };
   for (int g = wave; g < groups; g += kWaves) {
     const int first = s_first[g], end = s_first[g + 1];
@@ -214,10 +214,18 @@ __global__ __launch_bounds__(kPlanThreads) void prefix_plan_kernel(const PlanArg
     if (lane == 0) {
       s_keys[g] = keys;
       s_lead[g] = lead;
-      count(set_with(rows, 0, keys));
+      const Set s = set_with(rows, 0, keys);
+      const float cost = cost_of(s);
+      many_cost += s.many ? cost : 0.f;
+      others_cost += s.many ? 0.f : cost;
     }
     for (int b = first + lane; b < end; b += 64)
-      if (const int kv = s_kv[b]; kv > 0) count(set_with((s_cu[b + 1] - s_cu[b]) * a.group, keys, kv));
+      if (const int kv = s_kv[b]; kv > 0) {
+        const Set s = set_with((s_cu[b + 1] - s_cu[b]) * a.group, keys, kv);
+        const float cost = cost_of(s);
+        many_cost += s.many ? cost : 0.f;
+        others_cost += s.many ? 0.f : cost;
+      }
   }
   // (summed up in a fixed order, so that a batch has one plan)
   auto sum_over_wave = [](float x) {
