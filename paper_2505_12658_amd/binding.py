@@ -186,13 +186,18 @@ def hydra_page_maps_build(q_lens: torch.Tensor, context_lens: torch.Tensor, bloc
     if maps is None:
         batch = q_lens.numel()
 
-        def empty(n, dtype=torch.int32):
-            t = torch.empty(n, dtype=dtype, device=q_lens.device)
-            if stream is not None:
-                t.record_stream(stream)
-            return t
+        def allocate():
+            empty = lambda n, dtype=torch.int32: torch.empty(n, dtype=dtype, device=q_lens.device)  # noqa: E731
+            return PageMaps(empty(batch + 1), empty(batch), empty(total_tokens, torch.int64), empty(total_tokens), empty(batch), empty(2))
 
-        maps = PageMaps(empty(batch + 1), empty(batch), empty(total_tokens, torch.int64), empty(total_tokens), empty(batch), empty(2))
+        if stream is None:
+            maps = allocate()
+        else:  # memory of the stream that writes it, not handed out again before the current one is through
+            current = torch.cuda.current_stream(q_lens.device)
+            with torch.cuda.stream(stream):
+                maps = allocate()
+            for t in maps:
+                t.record_stream(current)
     _calls().page_maps_build(q_lens, context_lens, block_tables, free_blocks, n_free, total_tokens, block_size, num_blocks, position_deltas, *maps, stream)
     return maps
 

@@ -149,25 +149,41 @@ __global__ __launch_bounds__(kPlanThreads) void prefix_plan_kernel(const PlanArg
   int32_t* const s_at = s_lead + groups;        // [groups] first piece
   int32_t* const s_partial = s_at + groups;     // [sets] first row of its partial results, -1: final results
   int32_t* const s_parts = s_partial + sets;    // [sets] parts * 256 + rows of a block, 0: no pieces
-  __shared__ int32_t s_wave[3][kWaves];
+  __shared__ int32_t s_wave[3][kWaves], s_bad[kWaves];
   const int thread = (int)threadIdx.x, lane = thread & 63, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
   auto least = [](int x, int y) { return y < x ? y : x; };
 
+  bool bad = false;  // offsets that decrease or leave the batch, which rows and pieces would follow out of the workspace
   for (int i = thread; i <= batch; i += kPlanThreads) {
     const int at = a.cu_seqlens_q[i];
-    s_cu[i] = least(at < 0 ? 0 : at, a.total_q);
+    s_cu[i] = at;
+    bad |= at < 0 || at > a.total_q;
     if (i < batch) {
-      const int kv = a.kv_lens[i], end = a.cu_seqlens_q[i + 1], q = end - at;
+      const int kv = a.kv_lens[i], end = a.cu_seqlens_q[i + 1], q = (int)((uint32_t)end - (uint32_t)at);
       s_kv[i] = q > 0 && kv >= q ? least(kv, a.table_keys) : 0;
-      s_group[i] = 0;
+      bad |= end < at;
     }
   }
   for (int g = thread; g <= groups; g += kPlanThreads) {
     const int at = a.cu_groups[g];
-    s_first[g] = least(at < 0 ? 0 : at, batch);
-    if (g < groups) s_keys[g] = a.shared_lens[g];
+    s_first[g] = at;
+    bad |= at < 0 || at > batch || (g == 0 && at != 0) || (g == groups && at != batch);
+    if (g < groups) {
+      s_keys[g] = a.shared_lens[g];
+      bad |= a.cu_groups[g + 1] < at;
+    }
   }
+  if (const bool any = __builtin_amdgcn_ballot_w64(bad) != 0; lane == 0) s_bad[wave] = any;
   __syncthreads();
+  {
+    int32_t any = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) any |= s_bad[w];
+    if (any != 0) {
+      if (thread == 0) a.header->n_pieces = a.header->any_parts = 0;
+      return;
+    }
+  }
   auto set_with = [&](int rows, int begin, int end) {
     Set s;
     s.begin = begin;
@@ -324,7 +340,7 @@ __global__ __launch_bounds__(kPlanThreads) void prefix_plan_kernel(const PlanArg
     rows_before += rows_round;
     __syncthreads();
   }
-  // (there is room for all of them, unless offsets decrease)
+  // (there is room for all of them: see layout_of)
   const int all = many_before + others_before;
   const bool fits = all <= a.pieces_capacity && rows_before <= a.rows_capacity;
   if (thread == 0) {

@@ -12,6 +12,8 @@
 
 #include <ATen/ATen.h>
 #include <c10/core/DeviceGuard.h>
+#include <c10/core/StreamGuard.h>
+#include <c10/core/impl/VirtualGuardImpl.h>
 #include <c10/hip/HIPStream.h>
 #include <dlfcn.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -364,9 +366,11 @@ void* stream_on(PyObject* o, c10::Device device) {
   if (of != device.index()) raise(PyExc_ValueError, "stream must belong to the tensors' device");
   return stream_handle(o);
 }
-// Memory that the call allocated itself and uses on a stream that was given: not handed out again before that stream is through.
-void used_on(PyObject* o, const at::Tensor& t) {
-  if (o == Py_None || !t.defined()) return;
+// Memory for a call on a stream that was given (and checked by stream_on): that stream's own, so that nothing still uses it there, and
+// not handed out again before the current stream is through, where what the call returns may be read.
+template <typename F>
+at::Tensor allocated(PyObject* o, F&& make) {
+  if (o == Py_None) return make();
   int64_t field[3];
   const char* const names[3] = {"stream_id", "device_index", "device_type"};
   for (int i = 0; i < 3; ++i) {
@@ -376,7 +380,12 @@ void used_on(PyObject* o, const at::Tensor& t) {
     Py_DECREF(v);
     if (field[i] == -1 && PyErr_Occurred()) throw Raised{};
   }
-  t.record_stream(c10::Stream::unpack3(field[0], (c10::DeviceIndex)field[1], (c10::DeviceType)field[2]));
+  const c10::Stream given = c10::Stream::unpack3(field[0], (c10::DeviceIndex)field[1], (c10::DeviceType)field[2]);
+  const c10::Stream current = c10::impl::VirtualGuardImpl(given.device_type()).getStream(given.device());
+  const c10::StreamGuard guard(given);
+  at::Tensor t = make();
+  if (t.defined()) t.record_stream(current);
+  return t;
 }
 template <typename T>
 T* data(const at::Tensor* t) { return t ? static_cast<T*>(t->data_ptr()) : nullptr; }
@@ -447,12 +456,9 @@ PyObject* py_qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
     same_device(q, {&k, rotates ? positions : nullptr, freq, axis, q_weight, k_weight, v, kc, vc, slots});
     const c10::OptionalDeviceGuard guard(q.device());
+    void* s = stream_on(a[15], q.device());
     auto output = [&](PyObject* o, const at::Tensor& like, const char* name) {
-      if (o == Py_None) {
-        at::Tensor t = at::empty(like.sizes(), like.options().memory_format(c10::nullopt));
-        used_on(a[15], t);
-        return t;
-      }
+      if (o == Py_None) return allocated(a[15], [&] { return at::empty(like.sizes(), like.options().memory_format(c10::nullopt)); });
       const at::Tensor& t = token_major(o, name);
       if (t.sizes() != like.sizes()) raise(PyExc_ValueError, name, " must be shaped like its input");
       same_device(q, {&t});
@@ -465,7 +471,6 @@ PyObject* py_qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int64_t axis_stride = rotates && positions->dim() == 2 ? positions->stride(0) : 0;
     const int32_t rotary = rotates ? size32(2 * freq->numel()) : 0, total = size32(tokens), hq = size32(q.size(1)), hkv = size32(k.size(1)), dim = size32(d);
     const int32_t block = cached ? size32(kc->size(1)) : 1;
-    void* s = stream_on(a[15], q.device());
     call("hydra_qk_norm_rope", [&] {
       return lib.qk_norm_rope(q.data_ptr(), k.data_ptr(), cached ? v->data_ptr() : nullptr, q.stride(0), k.stride(0), cached ? v->stride(0) : 0, q_out.data_ptr(),
                               k_out.defined() ? k_out.data_ptr() : nullptr, q_out.stride(0), k_out.defined() ? k_out.stride(0) : 0, data<void>(q_weight), data<void>(k_weight), eps,
@@ -482,11 +487,7 @@ PyObject* py_qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 // A workspace that was given, or one of `need` bytes (of the least size where the sizes are refused anyway).
 at::Tensor workspace_of(PyObject* given, size_t need, const at::Tensor& with, PyObject* stream) {
-  if (given == Py_None) {
-    const at::Tensor t = bytes_on(with, std::max<size_t>(need, 16));
-    used_on(stream, t);
-    return t;
-  }
+  if (given == Py_None) return allocated(stream, [&] { return bytes_on(with, std::max<size_t>(need, 16)); });
   const at::Tensor& t = tensor(given, "workspace");
   if (!t.is_cuda() || !t.is_contiguous()) raise(PyExc_TypeError, "workspace must be a contiguous CUDA tensor");
   same_device(with, {&t});
@@ -503,8 +504,8 @@ PyObject* py_attn_prefix_plan(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int32_t batch = size32(kv.numel()), n_groups = size32(shared.numel()), total = whole(a[4]), hq = whole(a[5]), hkv = whole(a[6]), d = whole(a[7]), width = whole(a[8]),
                   block = whole(a[9]);
     const c10::OptionalDeviceGuard guard(cu.device());
-    const at::Tensor ws = workspace_of(a[10], lib.attn_prefix_workspace_bytes(batch, n_groups, total, hq, hkv, d), cu, a[11]);
     void* s = stream_on(a[11], cu.device());
+    const at::Tensor ws = workspace_of(a[10], lib.attn_prefix_workspace_bytes(batch, n_groups, total, hq, hkv, d), cu, a[11]);
     call("hydra_attn_prefix_plan", [&] {
       return lib.attn_prefix_plan(data<int32_t>(&cu), data<int32_t>(&kv), data<int32_t>(&groups), data<int32_t>(&shared), batch, n_groups, total, hq, hkv, d, width, block,
                                   ws.data_ptr(), ws.nbytes(), s);
@@ -530,9 +531,9 @@ struct Prefixed {
     width = size32(table.size(1));
   }
   at::Tensor output(PyObject* given, PyObject* stream) const {
+    if (given == Py_None) return allocated(stream, [&] { return out_like(given, q); });
     const at::Tensor t = out_like(given, q);
-    if (given == Py_None) used_on(stream, t);
-    else same_device(q, {&t});
+    same_device(q, {&t});
     return t;
   }
 };
@@ -549,9 +550,9 @@ PyObject* py_attn_prefix_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int32_t n_groups = size32(shared.numel());
     const float scale = (float)real(a[8]);
     const c10::OptionalDeviceGuard guard(p.q.device());
+    void* s = stream_on(a[11], p.q.device());
     const at::Tensor out = p.output(a[9], a[11]);
     const at::Tensor ws = workspace_of(a[10], a[10] == Py_None ? lib.attn_prefix_workspace_bytes(p.batch, n_groups, p.total, p.n_q, p.n_kv, p.d) : 0, p.q, a[11]);
-    void* s = stream_on(a[11], p.q.device());
     call("hydra_attn_prefix_fwd", [&] {
       return lib.attn_prefix_fwd(p.q.data_ptr(), out.data_ptr(), p.q.stride(0), p.kc.data_ptr(), p.vc.data_ptr(), data<int32_t>(&p.table), p.width, data<int32_t>(&cu),
                                  data<int32_t>(&kv), data<int32_t>(&groups), data<int32_t>(&shared), p.batch, n_groups, p.total, p.n_q, p.n_kv, p.d, p.block, p.kc.size(0), scale,
@@ -568,10 +569,10 @@ PyObject* py_attn_prefix_fwd_planned(PyObject*, PyObject* const* a, Py_ssize_t n
     const int32_t n_groups = whole(a[4]);
     const float scale = (float)real(a[5]);
     const c10::OptionalDeviceGuard guard(p.q.device());
+    void* s = stream_on(a[8], p.q.device());
     if (a[6] == Py_None) raise(PyExc_TypeError, "workspace must be the one that the plan was written into");
     const at::Tensor ws = workspace_of(a[6], 0, p.q, a[8]);
     const at::Tensor out = p.output(a[7], a[8]);
-    void* s = stream_on(a[8], p.q.device());
     call("hydra_attn_prefix_fwd_planned", [&] {
       return lib.attn_prefix_fwd_planned(p.q.data_ptr(), out.data_ptr(), p.q.stride(0), p.kc.data_ptr(), p.vc.data_ptr(), data<int32_t>(&p.table), p.width, p.batch, n_groups, p.total,
                                          p.n_q, p.n_kv, p.d, p.block, p.kc.size(0), scale, ws.data_ptr(), ws.nbytes(), s);

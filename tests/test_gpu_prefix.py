@@ -294,6 +294,70 @@ def test_workspaces_hold_the_plans_of_many_long_contexts(prefix, own, requests, 
         few.check(torch.cat([here, out[len(here): n]]))
 
 
+@both
+def test_all_keys_shared(planned):
+    """Several answers about to begin: contexts that are equal to the last key, which is the new token's own."""
+    batch = Batch([20, 2], [640, 128], [1] * 22, [1] * 22, 14, 2, 128, seed=12)
+    batch.kv_lens = [640] * 20 + [128] * 2
+    batch.check(_run(batch, planned))
+
+
+@pytest.mark.parametrize("sizes", [[2048], [1] * 2048, [0] * 1000 + [1024, 0, 1024] + [0] * 1045], ids=["one", "alone", "two"])
+@both
+def test_as_many_requests_and_groups_as_there_may_be(sizes, planned):
+    batch = Batch(sizes, [256] * len(sizes) if len(sizes) < 2048 or 0 in sizes else [3] * len(sizes), [1] * 2048, [1 + i % 37 for i in range(2048)], 2, 1, 64, seed=13)
+    batch.check(_run(batch, planned))
+
+
+@both
+def test_rows_behind_the_last_request_stay(planned):
+    batch = Batch([6], [512], [1, 2, 1, 0, 3, 1], [9, 2, 30, 1, 3, 70], 7, 1, 128, seed=14)
+    args = list(batch.on_gpu())
+    args[0] = torch.cat([args[0], torch.full((5, 7, 128), float("nan"), dtype=torch.bfloat16, device=DEV)])
+    out = torch.full_like(args[0], 3.0)
+    _call(planned, *args, out=out)
+    torch.cuda.synchronize()
+    batch.check(out[:8])
+    assert (out[8:] == 3.0).all()
+
+
+@pytest.mark.parametrize("name, values", [("cu", [0, 1, 9, 2, 3]), ("cu", [-1, 1, 2, 3, 4]), ("cu", [0, 1, 2, 3, 5]), ("groups", [0, 3, 2, 4]), ("groups", [0, 1, 3, 3]),
+                                          ("groups", [1, 2, 3, 4]), ("groups", [0, 2, 5, 4]), ("groups", [0, 2, 3, 5])])
+def test_plans_of_offsets_that_are_none(name, values):
+    """Offsets that decrease, or leave the batch: a plan without pieces."""
+    batch = Batch([1, 2, 1], [640, 640, 70], [1] * 4, [9, 2, 30, 1], 7, 1, 128, seed=15)
+    args = list(batch.on_gpu())
+    args[4 if name == "cu" else 6] = _i32(values)
+    out = torch.full_like(args[0], 3.0)
+    _call(True, *args, out=out)
+    torch.cuda.synchronize()
+    assert (out == 3.0).all()
+
+
+@both
+def test_a_stream_of_its_own(planned):
+    """On a side stream that is given as an argument, with outputs and workspaces that the calls allocate, while the current stream fills memory that it frees."""
+    import paper_2505_12658_amd as hydra
+
+    batch = Batch([12], [2048], [1] * 12, [9 + 5 * i for i in range(12)], 32, 32, 128, seed=5)
+    args = batch.on_gpu()
+    q, kc, vc, table, cu, kv, groups, shared, scale = args
+    need = hydra.hydra_attn_prefix_workspace_bytes(12, 1, 12, 32, 32, 128)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for _ in range(20):
+        torch.empty(need, dtype=torch.uint8, device=DEV).fill_(255)
+    if planned:
+        ws = hydra.hydra_attn_prefix_plan(cu, kv, groups, shared, 12, 32, 32, 128, table.shape[1], 16, stream=side)
+        out = hydra.hydra_attn_prefix_fwd_planned(q, kc, vc, table, 1, scale, ws, stream=side)
+    else:
+        out = hydra.hydra_attn_prefix_fwd(*args, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    batch.check(out)
+    with pytest.raises((TypeError, ValueError, AttributeError)):
+        hydra.hydra_attn_prefix_fwd(*args, stream=3)
+
+
 def test_binding_refuses_mismatched_tensors():
     import paper_2505_12658_amd as hydra
 
