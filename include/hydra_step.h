@@ -84,7 +84,7 @@ int hydra_page_maps_build(const int32_t* q_lens, const int32_t* context_lens, in
  *   q_out, k_out  the same with strides of their own; may be q and k themselves (same address, same stride), but overlap no other
  *             array.  k_out may be NULL with caches.
  *   q_weight, k_weight  bf16 [head_dim], 16-byte aligned, or NULL.  eps finite and >= 0.  The sum of squares is taken in fp32: values of
- *             2^60 and more in a row that is normalised overflow it.
+ *             2^60 and more in a row that is normalised overflow it, and with an eps below 2^-126 rows whose mean square is as small are taken as 0.
  *   positions device int32, axis a at positions + a * position_axis_stride, one per token; any int32.  A stride of 0 gives every axis
  *             the same positions.  n_axes 1 .. 4.
  *   inv_freq  device fp32 [R / 2], finite.   freq_axis  device int32 [R / 2], values clamped to 0 .. n_axes - 1, or NULL (all 0).

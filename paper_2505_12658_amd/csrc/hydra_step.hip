@@ -90,6 +90,7 @@ int hydra_qk_norm_rope(const void* q, const void* k, const void* v, int64_t q_to
     if (total_tokens > 0) return HYDRA_ERR_INVALID_ARG;
   }
   if (cached && (block_size < 1 || num_blocks < 0)) return HYDRA_ERR_INVALID_ARG;
+  if (cached && num_blocks > INT64_MAX / block_size) return HYDRA_ERR_UNSUPPORTED;
   if (rotary_dim > 0 && n_axes < 1) return HYDRA_ERR_INVALID_ARG;
   if (rotary_dim > 0 && n_axes > rope::kMostAxes) return HYDRA_ERR_UNSUPPORTED;
   if (total_tokens == 0) return HYDRA_OK;

@@ -358,6 +358,45 @@ def test_a_stream_of_its_own(planned):
         hydra.hydra_attn_prefix_fwd(*args, stream=3)
 
 
+FORMS = [([20, 3], [700, 130], [1 + 4 * (i % 2) for i in range(23)], [5 + 9 * i for i in range(23)], 32, 8, 128, 16),
+         ([9], [500], [1, 2, 9, 1, 1, 30, 1, 1, 70], [70, 3, 90, 1, 65, 31, 2, 200, 71], 14, 2, 128, 2),
+         ([20], [333], [1 + 4 * (i % 2) for i in range(20)], [5 + 9 * i for i in range(20)], 8, 2, 64, 64),
+         ([6], [200], [1, 7, 1, 40, 1, 1], [5, 60, 1, 40, 129, 64], 4, 2, 80, 16)]
+
+
+@pytest.mark.parametrize("case", FORMS, ids=lambda c: f"h{c[4]}k{c[5]}-d{c[6]}-b{c[7]}")
+@both
+def test_nothing_behind_the_contexts_is_used(case, planned):
+    """NaN in every row of the cache that is in no context: behind the last key in its block, and in blocks that nobody has."""
+    batch = Batch(*case, seed=16)
+    in_context = torch.zeros(batch.k_cache.shape[:2], dtype=torch.bool)
+    for row, n in zip(batch.tables, batch.kv_lens):
+        in_context[row[np.arange(n) // batch.block], np.arange(n) % batch.block] = True
+    want = batch.want(), batch.want(np.abs(_f64(batch.v_cache)))
+    batch.want = lambda values=None, q=None: want[values is not None]
+    for c in (batch.k_cache, batch.v_cache):
+        c[~in_context] = float("nan")
+    batch.check(_run(batch, planned))
+
+
+@pytest.mark.parametrize("case", FORMS[:1], ids=lambda c: f"h{c[4]}k{c[5]}-d{c[6]}-b{c[7]}")
+@both
+def test_blocks_behind_the_first_four_gigabytes(case, planned):
+    batch = Batch(*case, seed=17)
+    blocks, block, hkv, d = batch.k_cache.shape
+    apart = (5 << 30) // (block * hkv * d * 2) // blocks
+    far = torch.arange(blocks, device=DEV) * apart + apart - 1
+    args = list(batch.on_gpu())
+    for i in (1, 2):
+        wide = torch.zeros((blocks * apart, block, hkv, d), dtype=torch.bfloat16, device=DEV)
+        wide[far] = args[i]
+        args[i] = wide
+    args[3] = torch.where(args[3] < 0, args[3], args[3] * apart + apart - 1)
+    out = _call(planned, *args)
+    torch.cuda.synchronize()
+    batch.check(out)
+
+
 def test_binding_refuses_mismatched_tensors():
     import paper_2505_12658_amd as hydra
 

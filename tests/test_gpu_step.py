@@ -286,6 +286,18 @@ def test_slots_outside_the_cache_are_not_written():
     assert torch.equal(caches.cpu(), want)
 
 
+def test_slots_behind_the_first_four_gigabytes():
+    import paper_2505_12658_amd as hydra
+
+    q, k, v, _, _ = (t.to(DEV) for t in _draw(3, 5, 4, 8, 128))
+    slots = torch.tensor([2621500, 0, 2300000, 2621439, 17], device=DEV)  # (rows of 2 KB: 5.4 GB)
+    kc, vc = (torch.zeros((163900, 16, 8, 128), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    _, none = hydra.hydra_qk_norm_rope(q, k, None, None, v=v, k_cache=kc, v_cache=vc, slot_mapping=slots)
+    for cache, rows in ((kc, k), (vc, v)):
+        assert torch.equal(cache.view(-1, 8, 128)[slots], rows)
+        assert int((cache.view(-1, 1024) != 0).any(1).sum()) == 5
+
+
 def test_step_calls_on_a_stream_of_their_own():
     """Both calls, one after the other on a side stream that is given as an argument, allocating their outputs."""
     import paper_2505_12658_amd as hydra

@@ -59,7 +59,7 @@ def _rope(lib, q=16, k=16, v=16, qs=128, ks=128, vs=128, qo=32, ko=32, qos=128, 
     (dict(axis_stride=-8), INVALID), (dict(tokens=-1), INVALID), (dict(hq=0), INVALID), (dict(hkv=0), INVALID), (dict(rotary=-16), INVALID), (dict(rotary=80), INVALID),
     (dict(block=0), INVALID), (dict(blocks=-1), INVALID), (dict(qo=16, qos=256), INVALID), (dict(ko=16, kos=256), INVALID),
     (dict(axes=5), UNSUPPORTED), (dict(rotary=24), UNSUPPORTED), (dict(d=96), UNSUPPORTED), (dict(d=0), UNSUPPORTED), (dict(tokens=(1 << 25) + 1), UNSUPPORTED),
-    (dict(hq=65535, qs=1 << 23, qos=1 << 23), UNSUPPORTED), (dict(tokens=0), OK),
+    (dict(hq=65535, qs=1 << 23, qos=1 << 23), UNSUPPORTED), (dict(blocks=1 << 60), UNSUPPORTED), (dict(tokens=0), OK),
 ], ids=str)
 def test_norm_and_rotation_refusals(lib, change, status):
     assert _rope(lib, **change) == status
