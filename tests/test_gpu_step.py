@@ -62,6 +62,7 @@ def _maps_check(got, want):
     (1, 1, 0, 16, 0, 0), (1, 1, 31, 16, 0, 3), (3, 40, 50, 1, 0, 0), (5, 17, 33, 16, 4, 1), (64, 1, 700, 16, 0, 0), (65, 1, 700, 16, 3, 7), (130, 90, 300, 8, 0, 0),
     (200, 300, 10, 32, 200, 11), (1023, 1, 60, 4, 0, 0), (1024, 3, 60, 2, 5, 0), (1025, 9, 20, 16, 0, 1), (2500, 2, 90, 16, 9, 0), (40, 1200, 0, 16, 0, 5),
     (7, 5000, 3000, 64, 0, 0), (33, 2, 100, 256, 1, 40),
+    (256, 9, 30, 4, 0, 0), (257, 9, 30, 4, 2, 3), (900, 2000, 100, 16, 30, 7), (65535, 3, 40, 8, 0, 5),
 ])
 def test_page_maps(batch, q_most, context_most, block, lacking, more):
     q, context, tables, list_, free, total, blocks = _maps_case(batch * 7 + block, batch, q_most, context_most, block, lacking, more)
@@ -69,6 +70,20 @@ def test_page_maps(batch, q_most, context_most, block, lacking, more):
     args = (q, context, tables, list_, free, total, block, blocks)
     _maps_check(_maps_run(*args, deltas=deltas), reference.page_maps(*args, position_deltas=deltas))
     _maps_check(_maps_run(*args), reference.page_maps(*args))
+
+
+@pytest.mark.parametrize("batch, q_most, lacking", [(1500, 1, 0), (2300, 1, 40), (300, 50, 0), (1100, 400, 9)])
+def test_page_maps_of_large_batches_in_place(batch, q_most, lacking):
+    """Context lengths and free list overwritten by the call that reads them, in several rounds and several workgroups."""
+    import paper_2505_12658_amd as hydra
+
+    q, context, tables, list_, free, total, blocks = _maps_case(batch, batch, q_most, 90, 16, lacking)
+    e = lambda n, t=torch.int32: torch.empty(n, dtype=t, device=DEV)  # noqa: E731
+    table, d_context, pool = _i32(tables), _i32(context), _i32([free, 0])
+    maps = hydra.PageMaps(e(batch + 1), e(batch), e(total, torch.int64), e(total), d_context, pool)
+    hydra.hydra_page_maps_build(_i32(q), d_context, table, _i32(list_), pool, total, 16, blocks, maps=maps)
+    torch.cuda.synchronize()
+    _maps_check([t.cpu().numpy() for t in (*maps, table)], reference.page_maps(q, context, tables, list_, free, total, 16, blocks))
 
 
 def test_page_maps_of_lengths_that_do_not_fit():
