@@ -1,5 +1,20 @@
 // Attention over the paged cache of requests that share prefixes: the pieces of a plan (prefix_plan.hpp), and the merge of their
 // partial results.
+//
+// A row i of a piece meets keys j in begin .. end, as far as it sees them: with s_ij = q_i k_j, c = scale * log2(e) it leaves m_i (a reference for the row's
+// exponents, its maximum or a fixed one), l_i = sum_j 2^(c s_ij - m_i) and o_i = sum_j 2^(c s_ij - m_i) v_j.  Over the pieces p of a row, with M = max m_p, the result is
+// sum_p 2^(m_p - M) o_p / sum_p 2^(m_p - M) l_p.  Scores, m, l and o are fp32; the products take 2^(..) rounded to bf16, as those of the other attention calls do.
+//
+// Why pieces of a group's rows: a decode step's few query heads per KV head (7 of 28 / 4) leave the matrix instructions' tiles of 16 or 32 rows
+// half empty and read the prefix once per request; the rows of a group's requests fill blocks of 128 that read it once.  128 requests behind 16384 shared
+// keys, 28 / 4 heads of 128: 297 us request by request (every prefix 34 MB out of the caches, 14.6 TB/s), 53 us here, and 15 us for plan and merge.
+//
+// What bounds it there: the products, 900 TFLOP/s while both of a compute unit's workgroups have tiles (1.2 us a tile of 64 keys for 128 rows, each), and what a piece takes
+// besides its tiles, some 6 us from its start to the first product and in its last rows.  In small batches only that: 48 requests behind 4096 keys 16.5 us, of which a
+// piece of four tiles has 13, 4.7 until its first keys have come.
+//
+// Tried and slower: workgroups of eight waves, four of them loading (B of prefix_plan.hpp 74 us); one piece of many rows per compute unit (57 .. 63); a loop of
+// workgroups over the pieces instead of one workgroup each, also for those that the plan leaves empty (24 registers spilled: 58 and, in C, 24).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -32,7 +47,7 @@ __device__ __forceinline__ u32x2_t rounded(float a, float b, float c, float d) {
   return u32x2_t{__builtin_bit_cast(uint32_t, __builtin_convertvector(lo, bf16x2_t)), __builtin_bit_cast(uint32_t, __builtin_convertvector(hi, bf16x2_t))};
 }
 
-// ---- more than 64 rows: the packed kernel's pipeline (attn_fwd.hpp) --------------------------------------------------
+// ---- more than 32 rows: the packed kernel's pipeline (attn_fwd.hpp) --------------------------------------------------
 // A workgroup of four waves of 32 rows that share every tile of 64 keys.  The gatherer is the paged call's, from the piece's first key on.
 struct RowsSource {
   static constexpr bool kPaged = true, kOneItem = true, kPackedRows = true;
@@ -366,7 +381,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 #endif
 }
 
-// Merge: a wave per (token, query head), one after the other where there are more than waves.  A lane has two columns, so at head_dim 64
+// Merge: what bounds it is two trips to memory, and with many parts reading the partial results (B: 31 MB, 8.7 us; A 5.9, D 4.6).
+// A wave per (token, query head), one after the other where there are more than waves.  A lane has two columns, so at head_dim 64
 // the halves of the wave take every other partial result; kAtOnce results are asked for before the first is used.
 constexpr int kMergeWaves = 4, kMergeWorkgroups = 1024;
 template <int D>

@@ -6,7 +6,13 @@
 // rows and into parts of its keys; a piece is one block with one part, for every KV head, and a workgroup's work.  Where a row meets its
 // keys in several pieces, each leaves a partial result (maximum, sum, unnormalised output), and the merge puts them together.
 //
-// One workgroup plans: lengths and offsets of the whole batch lie in its LDS.  All sums are of whole numbers, so a batch has one plan.
+// One workgroup plans: lengths and offsets of the whole batch lie in its LDS.  All sums are of whole numbers or taken in a fixed order, so a batch has
+// one plan.  What bounds it: latency, of one trip to memory, some barriers and the pieces' writes: 48 requests 5.1 us, 128 6.4, 96 in 12 groups 5.8 (kPlanThreads
+// 256, 512, 1024: 48 requests 4.8, 5.1, 5.8, 96 in 12 groups, when a wave took each, 9.3, 7.6, 6.9).
+//
+// Figures in this file: us, decode steps with 28 / 4 heads of 128 (7 rows to a request) or 32 / 32 (one row); A: 48 requests behind 4096 keys, B: 128 behind 16384,
+// C: 96 in 12 groups behind 600 .. 1800, each with some hundreds of its own; D: 32 in 2 groups behind 1024, 32 / 32 heads.  Of the attention kernel alone,
+// which takes 16.5, 53, 18.7 and 24.8.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -27,15 +33,18 @@ constexpr int kSlots = 512;      // workgroups that the chip holds at once, two 
 
 // How a piece is computed (attn_prefix.hpp), and rows of a block.
 enum Form : int32_t { kFewRows = 0, kKeySplit = 1, kManyRows = 2 };
-// What takes which form: sets of up to 16 rows the first, up to kMostKeySplitRows the second.
+// What takes which form: sets of up to 16 rows the first, up to kMostKeySplitRows the second.  Without the first form (the second in its place) A 17.3, B 61.7, C 22.7,
+// D 30.1; without the third A 26.0, B 102, C 20.7; sets of 33 .. 64 rows in the second, D with 96 requests (48 rows) 51.7 instead of 49.6.
 constexpr int kMostKeySplitRows = 32;
 // Cost of a tile of keys for a block of rows, and of a piece whatever its keys, to scale: of many rows, and of others.  A tile of a full chip takes
 // 1.2 us for each workgroup.  kPieceCost 30, 45, 60, 80: 128 requests behind 16384 keys (28 / 4 heads of 128) 53.3, 53.6, 54.3, 57.2 us, 64 of them 33.1, 34.8, 35.3, 35.1,
 // 128 behind 8192 37.0, 36.5, 37.3, 39.5; kOtherTileCost 12, 8, 6: 96 in 12 groups behind 600 .. 1800 keys 18.3, 22.0, 22.8.
 constexpr int kTileCost = 16, kPieceCost = 30, kOtherTileCost = 12, kOtherPieceCost = 24;
-constexpr int kLeastTiles = 4, kOtherLeastTiles = 2;  // of a part: less is not worth a partial result
-constexpr int kOtherMostTiles = 4;                    // of a part of few rows, where there are partial results anyway
-constexpr int kPartialTiles = 32;                     // see the plan
+// Tiles of a part: less is not worth a partial result.  kLeastTiles 8: A 20.7, C 23.7, D alike; 2: A alike and its merge 0.6 more, 100 requests behind 1024 15.4
+// instead of 16.2 and their merge 0.4 more, with twice the partial results.
+constexpr int kLeastTiles = 4, kOtherLeastTiles = 2;
+constexpr int kOtherMostTiles = 4;  // of a part of few rows, where there are partial results anyway: 8 A 17.4, 2 and 4 alike
+constexpr int kPartialTiles = 32;   // see the plan: 16 and 64 alike in A .. D, whose groups are worth it by far
 
 struct Piece {
   int32_t table_row;            // request whose row of the block table the keys are found by
