@@ -5,7 +5,7 @@
 // a token then finds its request in LDS.  So one launch does, without a second one that would wait for the sums of a first: the
 // lengths are some KB that every workgroup after the first finds in L2.
 //
-// What bounds it: latency, of the lengths, the barriers and the table.  us: 96 decode steps 2.9, 700 3.7, 2000 5.9; prefills of 740 tokens, 100 3.5, 400
+// What bounds it: latency, of the lengths, the barriers and the table.  us: 96 decode steps 2.9, 700 3.7, 2000 5.9; prefills of 610 tokens, 100 3.5, 400
 // 5.4, 1024 (8 MB written) 8.2.  (Workgroups of 1024 threads with four tokens each: 4.6, 5.1, 9.9; 6.0, 8.0, 9.7.)
 #pragma once
 #include <hip/hip_runtime.h>
