@@ -397,6 +397,33 @@ def test_blocks_behind_the_first_four_gigabytes(case, planned):
     batch.check(out)
 
 
+@pytest.mark.parametrize("case", FORMS, ids=lambda c: f"h{c[4]}k{c[5]}-d{c[6]}-b{c[7]}")
+@both
+def test_a_scale_of_zero_takes_the_mean(case, planned):
+    batch = Batch(*case, seed=18)
+    batch.scale = 0.0
+    batch.check(_run(batch, planned))
+
+
+@pytest.mark.parametrize("case", FORMS, ids=lambda c: f"h{c[4]}k{c[5]}-d{c[6]}-b{c[7]}")
+@both
+def test_pages_outside_the_cache_harm_only_their_request(case, planned):
+    """Entries of one request's own blocks that no cache has: wrong numbers for it, and the others as they are without it."""
+    batch = Batch(*case, seed=19)
+    bad = 4
+    first = batch.prefixes[0] // batch.block
+    args = list(batch.on_gpu())
+    table = batch.tables.copy()
+    table[bad, first: -(-batch.kv_lens[bad] // batch.block)] = [-7, 2 ** 31 - 1, 10 ** 6][bad % 3]
+    args[3] = _i32(table)
+    out = _call(planned, *args)
+    torch.cuda.synchronize()
+    assert torch.isfinite(out).all()
+    mine = slice(batch.cu[bad], batch.cu[bad + 1])
+    out[mine] = _run(batch, planned)[mine]
+    batch.check(out)
+
+
 def test_binding_refuses_mismatched_tensors():
     import paper_2505_12658_amd as hydra
 
