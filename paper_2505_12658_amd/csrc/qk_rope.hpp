@@ -12,7 +12,7 @@
 //
 // What bounds it: HBM, each row is read once and written once; with a handful of tokens the two trips to memory.  30 000 tokens of 28 / 4 heads of
 // 128 with the cache write 98 us (5.65 TB/s read and written, where a copy of a GB reaches 5.14), with norms 101.5; heads of 64 55 and 62; 65 536 tokens of 16
-// heads of 80 125 us (5.4 TB/s), with norms 150, which the sums over five lanes take; 4 tokens 3.5, 256 of 32 / 32 heads 3.5.
+// heads of 80 124 us (5.4 TB/s), with norms 135 (fewer waves at once, and the sums over five lanes); 4 tokens 3.5, 256 of 32 / 32 heads 3.5.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -26,9 +26,9 @@ constexpr int kMostAxes = 4;
 constexpr int kWaves = 4;      // of a workgroup
 // Rows that a lane has loaded before it computes.  us with 1, 2 and 4: 28 / 4 heads of 128 with the cache write, 30 000 tokens 98, 97, 98, with
 // norms (when their root was two instructions) 105, 103, 120; 4 tokens 3.6, 3.9, 4.7; heads of 64, 30 000 tokens 55 whatever, with norms 64, 67, 67.  16 heads of 80, whose
-// rows leave a wave's lanes with three at a time: 65 536 tokens with 1, 2, 3, 4: 129, 127, 124, 126.
-template <int D>
-constexpr int kRowsInFlight = D == 80 ? 3 : 1;
+// rows leave a wave's lanes with three at a time: 65 536 tokens with 1, 2, 3, 4: 129, 127, 124, 126; with norms 135, 149, 137.
+template <int D, bool NORM>
+constexpr int kRowsInFlight = D == 80 && !NORM ? 3 : 1;
 
 struct Args {
   const uint16_t *q, *k, *v;
@@ -115,19 +115,13 @@ __global__ __launch_bounds__(64 * kWaves) void qk_norm_rope_kernel(const Args a)
   const int rp = a.rotary_pieces;
   const bool rotates = piece < rp;
   const int l = rotates ? piece : 2 * rp + (piece - rp), u = rotates ? piece + rp : PIECES + piece;
-  float w_q[16], w_k[16];
+  u32x4_t w_q[2], w_k[2];  // (as bf16: as fp32 they are 16 registers more, and at head_dim 80 a wave less to a SIMD, 146 us instead of 137)
   if constexpr (NORM) {
     const u32x4_t ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
-    auto weights = [&](const uint16_t* w, float (&to)[16]) {
+    auto weights = [&](const uint16_t* w, u32x4_t (&to)[2]) {
       const bool there = active && w != nullptr;
-      const u32x4_t wl = there ? reinterpret_cast<const u32x4_t*>(w)[l] : ones, wu = there ? reinterpret_cast<const u32x4_t*>(w)[u] : ones;
-      float x[8];
-      unpack(wl, x);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) to[i] = x[i];
-      unpack(wu, x);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) to[8 + i] = x[i];
+      to[0] = there ? reinterpret_cast<const u32x4_t*>(w)[l] : ones;
+      to[1] = there ? reinterpret_cast<const u32x4_t*>(w)[u] : ones;
     };
     weights(a.q_weight, w_q);
     weights(a.k_weight, w_k);
@@ -146,11 +140,11 @@ __global__ __launch_bounds__(64 * kWaves) void qk_norm_rope_kernel(const Args a)
   f32x2_t* const angles = reinterpret_cast<f32x2_t*>(s_angles[threadIdx.x >> 6]);
   f32x2_t angle[8];  // of this lane's pairs
   bool have_angles = false;
-  for (int row0 = part * a.rows_per_part; row0 < row_end; row0 += ROWS * kRowsInFlight<D>) {
-    u32x4_t low[kRowsInFlight<D>], up[kRowsInFlight<D>];
+  for (int row0 = part * a.rows_per_part; row0 < row_end; row0 += ROWS * kRowsInFlight<D, NORM>) {
+    u32x4_t low[kRowsInFlight<D, NORM>], up[kRowsInFlight<D, NORM>];
     auto row_of = [&](int i) { return row0 + i * ROWS + lane_row; };
 #pragma unroll
-    for (int i = 0; i < kRowsInFlight<D>; ++i) {
+    for (int i = 0; i < kRowsInFlight<D, NORM>; ++i) {
       const int row = row_of(i);
       if (active && row < row_end) {
         const uint16_t* from = row < k_first ? q_in + (int64_t)row * D : row < v_first ? k_in + (int64_t)(row - k_first) * D : v_in + (int64_t)(row - v_first) * D;
@@ -186,7 +180,7 @@ __global__ __launch_bounds__(64 * kWaves) void qk_norm_rope_kernel(const Args a)
       }
     }
 #pragma unroll
-    for (int i = 0; i < kRowsInFlight<D>; ++i) {
+    for (int i = 0; i < kRowsInFlight<D, NORM>; ++i) {
       const int row = row_of(i);
       const bool there = active && row < row_end, is_v = row >= v_first;
       float x[8], y[8];
@@ -203,10 +197,13 @@ __global__ __launch_bounds__(64 * kWaves) void qk_norm_rope_kernel(const Args a)
         const bool is_q = row < k_first;
         const bool normed = is_q ? a.q_weight != nullptr : a.k_weight != nullptr;
         const float scale = normed ? __builtin_amdgcn_rsqf(squares * (1.0f / D) + a.eps) : 1.0f;
+        float wx[8], wy[8];
+        unpack(is_q ? w_q[0] : w_k[0], wx);
+        unpack(is_q ? w_q[1] : w_k[1], wy);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          x[j] = x[j] * scale * (is_q ? w_q[j] : w_k[j]);
-          y[j] = y[j] * scale * (is_q ? w_q[8 + j] : w_k[8 + j]);
+          x[j] = x[j] * scale * wx[j];
+          y[j] = y[j] * scale * wy[j];
         }
       }
       float xr[8], yr[8];
