@@ -424,6 +424,32 @@ def test_pages_outside_the_cache_harm_only_their_request(case, planned):
     batch.check(out)
 
 
+@both
+def test_two_recorded_steps_share_a_workspace(planned):
+    """Two batches of different sizes, each recorded with its plan, replayed in turn over one workspace."""
+    import paper_2505_12658_amd as hydra
+
+    batches = [Batch([12], [2048], [1] * 12, [9 + 5 * i for i in range(12)], 32, 32, 128, seed=20), Batch([5, 20], [320, 700], [1] * 20 + [2] * 5, [9 + 7 * i for i in range(25)], 28, 4, 128, seed=21)]
+    need = max(hydra.hydra_attn_prefix_workspace_bytes(len(b.kv_lens), len(b.sizes), b.q.shape[0], b.hq, b.hkv, b.d) for b in batches)
+    ws = torch.empty(need, dtype=torch.uint8, device=DEV)
+    steps = []
+    for b in batches:
+        args = b.on_gpu()
+        out = torch.zeros_like(args[0])
+        eager = _call(planned, *args, workspace=ws).clone()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            _call(planned, *args, out=out, workspace=ws)
+        b.check(eager)
+        steps.append((graph, out, eager, args))
+    for _ in range(3):
+        for graph, out, eager, _ in steps:
+            out.fill_(7.0)
+            graph.replay()
+            assert torch.equal(out.view(torch.int16), eager.view(torch.int16))
+
+
 def test_binding_refuses_mismatched_tensors():
     import paper_2505_12658_amd as hydra
 
