@@ -381,14 +381,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 #endif
 }
 
-// Merge: what bounds it is two trips to memory, and with many parts reading the partial results (B: 31 MB, 8.7 us; A 5.9, D 4.6).
+// Merge: what bounds it is two trips to memory, and with many parts reading the partial results (B: 31 MB, 8.8 us; A 5.2, C 4.7, D 4.6; with kAtOnce
+// 4, 8, 12 B 8.0, 8.5, 9.0, A 6.2, 5.7, 5.6).
 // A wave per (token, query head), one after the other where there are more than waves.  A lane has two columns, so at head_dim 64
-// the halves of the wave take every other partial result; kAtOnce results are asked for before the first is used.
+// the halves of the wave take every other partial result; two times kAtOnce results are asked for before the first is used.
 constexpr int kMergeWaves = 4, kMergeWorkgroups = 1024;
 template <int D>
 __global__ __launch_bounds__(64 * kMergeWaves) void prefix_merge_kernel(const Args a) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  constexpr int kStreams = D == 64 ? 2 : 1, kEach = 2 * kMostParts / 64, kAtOnce = 12;
+  constexpr int kStreams = D == 64 ? 2 : 1, kEach = 2 * kMostParts / 64, kAtOnce = 6;
   const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n_heads = a.paged.n_q_heads, group = a.paged.group, batch = a.paged.batch;
   const int units = a.total_q * n_heads, first_unit = (int)blockIdx.x * kMergeWaves + wave;
@@ -450,6 +451,8 @@ __global__ __launch_bounds__(64 * kMergeWaves) void prefix_merge_kernel(const Ar
       const int i = e * 64 + lane;
       stat[e] = *reinterpret_cast<const f32x2_t*>(a.stats + 2 * row_of(i < n ? i : n - 1));
     }
+    constexpr int kStep = kAtOnce * kStreams;
+    if (kStep < n) load(v[1], kStep);
     float top = stat[0][0];
 #pragma unroll
     for (int e = 1; e < kEach; ++e) top = fmaxf(top, stat[e][0]);
@@ -479,12 +482,11 @@ __global__ __launch_bounds__(64 * kMergeWaves) void prefix_merge_kernel(const Ar
         acc[1] += w * from[u][1];
       }
     };
-    constexpr int kStep = kAtOnce * kStreams;
     for (int i0 = 0; i0 < n; i0 += 2 * kStep) {
-      if (i0 + kStep < n) load(v[1], i0 + kStep);
       add(v[0], i0);
       if (i0 + 2 * kStep < n) load(v[0], i0 + 2 * kStep);
       add(v[1], i0 + kStep);
+      if (i0 + 3 * kStep < n) load(v[1], i0 + 3 * kStep);
     }
     if constexpr (kStreams == 2) {
       acc[0] += __shfl_xor(acc[0], 32);
